@@ -1,0 +1,370 @@
+"""Three groups of operators between a layer's projections and its attention, as calls and in plain form.
+
+``qk``      per-head RMS norm of queries and keys with the rotation by (time, height, width) in the same
+            pass, out of a fused projection's rows into the attention's query rows and the K/V slots.
+``pack``    rows of the K/V cache to 4 bits and back to the values these stand for: what a chunk commit does
+            to the clean region (with ``kept``, the rows that a selection kept, which lie anywhere).
+``unpack``  cached 4-bit rows to the cache's own type: what a commit does before it scores the keys.
+``attend``  chunk-causal attention on a clean region held in 4 bits and the active chunks' slots.
+
+The shapes are those of the repository's workloads: a MAGI-1-like layer (24 x 128, chunks of 6 x 30 x 52 = 9360
+tokens), a SkyReels-V2-1.3B-like layer (12 x 128, chunks of 5 x 34 x 60 = 10200 tokens), the tiny fp32 step of the
+smoke test and the reduced ragged shapes of the tests.
+"""
+import math
+
+import torch
+
+own = False
+
+DEV = "cuda"
+DTYPES = {"bf16": torch.bfloat16, "f32": torch.float32}
+THETA, EPS = 10000.0, 1e-6
+
+
+def _qk(name, dtype, H_q, H_k, d, A, R, L_c, L_clean, grid_h, grid_w, frame0, pairing):
+    return {"name": name, "kind": "qk", "dtype": dtype, "H_q": H_q, "H_k": H_k, "d": d, "A": A, "R": R, "L_c": L_c,
+            "L_clean": L_clean, "grid_h": grid_h, "grid_w": grid_w, "frame0": frame0, "pairing": pairing}
+
+
+def _pack(name, dtype, H, d, L, count, kept):
+    return {"name": name, "kind": "pack", "dtype": dtype, "H": H, "d": d, "L": L, "count": count, "kept": kept}
+
+
+def _unpack(name, dtype, H, d, L, count):
+    return {"name": name, "kind": "unpack", "dtype": dtype, "H": H, "d": d, "L": L, "count": count}
+
+
+def _attend(name, H_q, H_k, d, A, R, L_c, L_clean, reverse=False):
+    return {"name": name, "kind": "attend", "dtype": "bf16", "H_q": H_q, "H_k": H_k, "d": d, "A": A, "R": R, "L_c": L_c,
+            "L_clean": L_clean, "reverse": reverse}
+
+
+def listed():
+    return [
+        # the smoke test's layer: launches count
+        _qk("qk tiny f32", "f32", 4, 1, 64, 2, 1, 128, 512, 8, 16, 0, "interleaved"),
+        # a reduced grouped layer whose chunk ends inside a frame
+        _qk("qk small grouped", "bf16", 8, 2, 128, 2, 1, 328, 984, 7, 9, 40, "interleaved"),
+        # most recomputing ticks: only the newest chunk, late in a long video
+        _qk("qk skyreels newest", "bf16", 12, 12, 128, 2, 1, 10200, 0, 34, 60, 1275, "interleaved"),
+        # every chunk recomputed, after a clean region in the same cache
+        _qk("qk magi all", "bf16", 24, 24, 128, 4, 4, 9360, 9360, 30, 52, 96, "halves"),
+        # commit of a reduced fp32 layer
+        _pack("pack small f32", "f32", 4, 64, 1312, 983, True),
+        # commit at full length: the kept half of the cache
+        _pack("pack magi kept", "bf16", 24, 128, 74880, 37440, True),
+        # the rows of a reduced layer's clean region, part of a longer buffer
+        _unpack("unpack small", "bf16", 12, 64, 1311, 1001),
+        # the clean region of five chunks before its keys are scored
+        _unpack("unpack skyreels", "bf16", 12, 128, 51000, 51000),
+        # a single query row on a long cache
+        _attend("attend one row", 12, 12, 128, 1, 1, 1, 61201),
+        # a reduced grouped layer
+        _attend("attend small grouped", 8, 2, 128, 2, 1, 328, 1311),
+        # a window of five frame-sized chunks at head dimension 64, slots in a ring's order
+        _attend("attend d64 window", 24, 24, 64, 5, 2, 2040, 18360, reverse=True),
+        # the SkyReels-like layer's newest chunk on a full budget
+        _attend("attend skyreels newest", 12, 12, 128, 2, 1, 10200, 40800),
+    ]
+
+
+def _log(rng, lo, hi):
+    return int(round(math.exp(rng.uniform(math.log(lo), math.log(hi)))))
+
+
+def draw(rng):
+    """One more case of the ranges above; lengths are odd as often as not."""
+    kind = rng.choice(("qk", "pack", "unpack", "attend", "attend"))
+    d = rng.choice((64, 128, 128))
+    H_k = rng.choice((1, 2, 4, 8, 12, 12, 24))
+    H_q = H_k * rng.choice((1, 1, 1, 2, 4)) if H_k <= 8 else H_k
+    dtype = "bf16" if rng.random() < 0.75 else "f32"
+    if kind == "qk":
+        A = rng.choice((1, 2, 2, 3, 4, 4))
+        L_c = _log(rng, 1, 9360 if dtype == "bf16" else 4000)
+        return _plain(_qk("", dtype, H_q if H_k <= 4 else H_k, H_k, d, A, rng.randint(1, A), L_c, rng.choice((0, rng.randint(1, 9360))),
+                          rng.randint(1, 34), rng.randint(1, 60), _log(rng, 1, 60000), rng.choice(("interleaved", "halves"))))
+    if kind in ("pack", "unpack"):
+        L = _log(rng, 600, 60000 if dtype == "bf16" else 30000)
+        count = max(1, int(L * rng.uniform(0.4, 1.0)))
+        return _plain(_pack("", dtype, H_k, d, L, min(count, 37440), rng.random() < 0.6) if kind == "pack" else
+                      _unpack("", dtype, H_k, d, L, min(count, 51000)))
+    while True:
+        A = rng.choice((1, 2, 2, 3, 4, 4, 6))
+        c = _attend("", H_q, H_k, d, A, rng.randint(1, A), _log(rng, 1, 10200), _log(rng, 1, 61200), rng.random() < 0.3)
+        if H_q * A * c["L_c"] * (c["L_clean"] + A * c["L_c"]) <= 7.6e9:      # the plain form's table of scores
+            return _plain(c)
+
+
+def _plain(case):
+    del case["name"]
+    return case
+
+
+def axis_dims(d):
+    """Shares of the head dimension that time, height and width rotate."""
+    side = 2 * (d // 6)
+    return (d - 2 * side, side, side)
+
+
+def _generator(seed):
+    g = torch.Generator(device=DEV)
+    g.manual_seed(seed)
+    return g
+
+
+def _normal(g, shape, dtype):
+    return torch.randn(shape, generator=g, device=DEV, dtype=torch.float32).to(dtype)
+
+
+def _values(packed, H, capacity, d):
+    """fp32 values [H, capacity, d] of a 4-bit buffer: two e2m1 codes a byte (the even element low), then one
+    power-of-two scale byte (bias 127) for every 32 elements."""
+    grid = torch.tensor([0, .5, 1, 1.5, 2, 3, 4, 6, 0, -.5, -1, -1.5, -2, -3, -4, -6], device=packed.device)
+    codes = packed[:H * capacity * d // 2].view(H, capacity, d // 2)
+    scales = packed[H * capacity * d // 2:].view(H, capacity, d // 32, 1)
+    v = torch.stack((grid[(codes & 15).long()], grid[(codes >> 4).long()]), -1).view(H, capacity, d // 32, 32)
+    return (v * torch.exp2(scales.float() - 127)).view(H, capacity, d)
+
+
+def _to4(x):
+    """4-bit buffer of fp32 rows [H, n, d]: the scale is a quarter of the largest magnitude's power of two, or half of it
+    from 1.75 times that power on; codes to nearest, ties to even."""
+    H, n, d = x.shape
+    b = x.view(H, n, d // 32, 32)
+    m, k = torch.frexp(b.abs().amax(-1, keepdim=True))
+    e = (k - 3 + (m >= 0.875)).clamp(-126, 125)
+    a = torch.ldexp(b, -e)
+    s = a.abs()
+    code = ((s > .25).to(torch.uint8) + (s >= .75) + (s > 1.25) + (s >= 1.75) + (s > 2.5) + (s >= 3.5) + (s > 5.)
+            + 8 * (a < 0)).view(H, n, d // 2, 2)
+    return torch.cat(((code[..., 0] | code[..., 1] << 4).reshape(-1), (e + 127).to(torch.uint8).reshape(-1)))
+
+
+def prepare(case, seed):
+    g = _generator(seed)
+    dtype, d = DTYPES[case["dtype"]], case["d"]
+    s = {"case": case}
+    if case["kind"] in ("qk", "attend"):
+        A, R, L_c, L_clean = case["A"], case["R"], case["L_c"], case["L_clean"]
+        H_q, H_k = case["H_q"], case["H_k"]
+        # the newest R chunks recompute
+        s["idx"] = torch.tensor(list(range(A - R, A)) + [-1] * (A - R), dtype=torch.int32, device=DEV)
+        s["n"] = torch.tensor([R], dtype=torch.int32, device=DEV)
+    if case["kind"] == "qk":
+        # one fused projection's rows: queries, keys, values; a trained norm's weights lie around one
+        s["qkv"] = _normal(g, (A * L_c, H_q + 2 * H_k, d), dtype)
+        s["wq"], s["wk"] = (1.0 + 0.2 * _normal(g, (d,), torch.float32) for _ in range(2))
+        s["off"] = [L_clean + i * L_c for i in range(A)]
+        s["k_cache"] = _normal(g, (H_k, L_clean + A * L_c, d), dtype)
+        s["v_cache"] = _normal(g, (H_k, L_clean + A * L_c, d), dtype)
+        s["q_out"] = torch.zeros((A * L_c, H_q, d), dtype=dtype, device=DEV)
+        frames = -(-L_c // (case["grid_h"] * case["grid_w"]))
+        s["frame0"] = [case["frame0"] + i * frames for i in range(A)]
+    elif case["kind"] == "pack":
+        H, L, n = case["H"], case["L"], case["count"]
+        s["k_cache"], s["v_cache"] = _normal(g, (H, L, d), dtype), _normal(g, (H, L, d), dtype)
+        s["kept"] = None
+        if case["kept"]:
+            score = torch.rand((H, L), generator=g, device=DEV)
+            s["kept"] = score.topk(n, 1).indices.sort(1).values.to(torch.int32).contiguous()
+        s["k4"], s["v4"] = (torch.zeros(H * n * (d // 2 + d // 32), dtype=torch.uint8, device=DEV) for _ in range(2))
+        s["k_back"], s["v_back"] = (torch.zeros((H, n, d), dtype=dtype, device=DEV) for _ in range(2))
+    elif case["kind"] == "unpack":
+        H, L, n = case["H"], case["L"], case["count"]
+        s["k4"], s["v4"] = (_to4(_normal(g, (H, L, d), torch.float32)) for _ in range(2))
+        s["k_back"], s["v_back"] = (torch.zeros((H, n, d), dtype=dtype, device=DEV) for _ in range(2))
+    else:
+        # keys that went through a norm have entries of unit size
+        s["q"] = _normal(g, (A * L_c, H_q, d), dtype)
+        s["k4"], s["v4"] = (_to4(_normal(g, (H_k, L_clean, d), torch.float32)) for _ in range(2))
+        s["k_cache"], s["v_cache"] = (_normal(g, (H_k, A * L_c, d), dtype) for _ in range(2))
+        s["off"] = [i * L_c for i in range(A)]
+        if case["reverse"]:
+            s["off"].reverse()
+        s["out"] = torch.zeros_like(s["q"])
+    # the lists' own copies on the GPU, for the plain forms' indexing
+    s["dims"] = axis_dims(d)
+    for name in ("off", "frame0", "dims"):
+        if name in s:
+            s[name + "_gpu"] = torch.tensor(s[name], device=DEV)
+    return s
+
+
+def run(s):
+    case = s["case"]
+    return {"qk": _run_qk, "pack": _run_pack, "unpack": _run_unpack, "attend": _run_attend}[case["kind"]](s, case)
+
+
+def _run_qk(s, c):
+    H_q, H_k, d, R, L_c = c["H_q"], c["H_k"], c["d"], c["R"], c["L_c"]
+    q, k, v = s["qkv"].split((H_q, H_k, H_k), 1)
+    if own:
+        from paper_2602_10825_amd import binding as B
+        B.flowcache_qk_norm_rope(q, k, v, s["k_cache"], s["v_cache"], L_c, c["L_clean"], s["off"], s["idx"], s["n"],
+                                 axis_dims(d), (c["grid_h"], c["grid_w"]), s["frame0"], THETA, c["pairing"],
+                                 s["wq"], s["wk"], EPS, q_out=s["q_out"])
+    else:
+        rows = R * L_c
+        chunk = s["idx"][:R].long().repeat_interleave(L_c)
+        n = torch.arange(L_c, device=DEV).repeat(R)
+        first, off = s["frame0_gpu"], s["off_gpu"]
+        hw = c["grid_h"] * c["grid_w"]
+        pos = torch.stack((first[chunk] + n // hw, n // c["grid_w"] % c["grid_h"], n % c["grid_w"]), 1).double()
+        dims = s["dims_gpu"]
+        axis = torch.arange(3, device=DEV).repeat_interleave(dims // 2)
+        i = torch.arange(d // 2, device=DEV) - (torch.cumsum(dims // 2, 0) - dims // 2)[axis]
+        angle = pos[:, axis] * THETA ** (-2.0 * i.double() / dims[axis])       # 64 bits: far frames turn many times
+        cos, sin = angle.cos().float()[:, None], angle.sin().float()[:, None]
+
+        def turned(x, w):
+            x = x[:rows].float()
+            x = x * torch.rsqrt((x * x).mean(-1, keepdim=True) + EPS) * w
+            if c["pairing"] == "halves":
+                a, b = x[..., :d // 2], x[..., d // 2:]
+                return torch.cat((a * cos - b * sin, a * sin + b * cos), -1).to(q.dtype)
+            a, b = x[..., 0::2], x[..., 1::2]
+            return torch.stack((a * cos - b * sin, a * sin + b * cos), -1).flatten(-2).to(q.dtype)
+
+        at = off[chunk] + n
+        s["q_out"][:rows] = turned(q, s["wq"])
+        s["k_cache"][:, at] = turned(k, s["wk"]).transpose(0, 1)
+        s["v_cache"][:, at] = v[:rows].transpose(0, 1)
+    return {"q": s["q_out"], "k": s["k_cache"], "v": s["v_cache"]}
+
+
+def _run_pack(s, c):
+    H, d, n = c["H"], c["d"], c["count"]
+    if own:
+        from paper_2602_10825_amd import binding as B
+        B.flowcache_kv4_pack(s["k_cache"], s["v_cache"], s["k4"], s["v4"], n, n, kept_idx=s["kept"])
+        B.flowcache_kv4_unpack(s["k4"], s["v4"], n, s["k_back"], s["v_back"], n)
+        return {"k": s["k_back"], "v": s["v_back"]}
+    rows = torch.arange(n, device=DEV).expand(H, n) if s["kept"] is None else s["kept"].long()
+    head = torch.arange(H, device=DEV)[:, None]
+    s["k4"].copy_(_to4(s["k_cache"][head, rows].float()))
+    s["v4"].copy_(_to4(s["v_cache"][head, rows].float()))
+    s["k_back"].copy_(_values(s["k4"], H, n, d))
+    s["v_back"].copy_(_values(s["v4"], H, n, d))
+    return {"k": s["k_back"], "v": s["v_back"]}
+
+
+def _run_unpack(s, c):
+    n = c["count"]
+    if own:
+        from paper_2602_10825_amd import binding as B
+        B.flowcache_kv4_unpack(s["k4"], s["v4"], c["L"], s["k_back"], s["v_back"], n)
+    else:
+        s["k_back"].copy_(_values(s["k4"], c["H"], c["L"], c["d"])[:, :n])
+        s["v_back"].copy_(_values(s["v4"], c["H"], c["L"], c["d"])[:, :n])
+    return {"k": s["k_back"], "v": s["v_back"]}
+
+
+def _run_attend(s, c):
+    H_q, H_k, d, A, R, L_c, L = c["H_q"], c["H_k"], c["d"], c["A"], c["R"], c["L_c"], c["L_clean"]
+    if own:
+        from paper_2602_10825_amd import binding as B
+        return B.flowcache_attend_kv4(s["q"], None, None, s["k4"], s["v4"], L, s["k_cache"], s["v_cache"], L_c, L, s["off"],
+                                      s["idx"], s["n"], out=s["out"], want_lse=False)["out"]
+    rows, group = R * L_c, H_q // H_k
+    k = torch.cat((_values(s["k4"], H_k, L, d), s["k_cache"].float()), 1)
+    v = torch.cat((_values(s["v4"], H_k, L, d), s["v_cache"].float()), 1)
+    # chunk of every key (clean ones come before all) and of every query row
+    key_chunk = torch.cat((torch.full((L,), -1, device=DEV), s["off_gpu"].argsort().repeat_interleave(L_c)))
+    row_chunk = s["idx"][:R].repeat_interleave(L_c)
+    q = s["q"][:rows].float().view(rows, H_k, group, d).permute(1, 2, 0, 3).reshape(H_k, group * rows, d)
+    t = torch.matmul(q, k.transpose(1, 2).contiguous()).view(H_q, rows, -1)
+    t.mul_(d ** -0.5).masked_fill_(key_chunk > row_chunk[:, None], -math.inf)
+    t.sub_(t.amax(-1, keepdim=True)).exp_()
+    total = t.sum(-1, keepdim=True)
+    o = torch.matmul(t.view(H_k, group * rows, -1), v).view(H_q, rows, d) / total
+    s["out"][:rows] = o.transpose(0, 1).to(s["out"].dtype)
+    return s["out"]
+
+
+def work(case):
+    e, d = 2 if case["dtype"] == "bf16" else 4, case["d"]
+    row4 = d // 2 + d // 32
+    if case["kind"] == "qk":
+        # queries, keys and values in, and each once out; square, scale and rotation of queries and keys
+        rows = case["R"] * case["L_c"]
+        return {"bytes": 2 * rows * (case["H_q"] + 2 * case["H_k"]) * d * e, "flops": 8 * rows * (case["H_q"] + case["H_k"]) * d}
+    if case["kind"] == "pack":
+        # K and V in, 4-bit rows out; then those in again and their values out
+        rows = 2 * case["H"] * case["count"]
+        return {"bytes": 2 * rows * (d * e + row4) + (4 * case["H"] * case["count"] if case["kept"] else 0), "flops": 4 * rows * d}
+    if case["kind"] == "unpack":
+        rows = 2 * case["H"] * case["count"]
+        return {"bytes": rows * (d * e + row4), "flops": rows * d}
+    A, R, L_c, L, H_q, H_k = (case[k] for k in ("A", "R", "L_c", "L_clean", "H_q", "H_k"))
+    seen = [L + (c + 1) * L_c for c in range(A - R, A)]
+    return {"bytes": 2 * H_k * (L * row4 + A * L_c * d * e) + 2 * R * L_c * H_q * d * e, "flops": 4 * H_q * d * L_c * sum(seen)}
+
+
+def exact(case, seed):
+    """What run() returns for these inputs, in 64 bits, from the definitions."""
+    s, d = prepare(case, seed), case["d"]
+    if case["kind"] == "qk":
+        q, k, v = (x.double() for x in s["qkv"].split((case["H_q"], case["H_k"], case["H_k"]), 1))
+        out, kc, vc = s["q_out"].double(), s["k_cache"].double(), s["v_cache"].double()
+        L_c = case["L_c"]
+        n = torch.arange(L_c, dtype=torch.float64, device=DEV)
+        hw = case["grid_h"] * case["grid_w"]
+        for r, c in enumerate(range(case["A"] - case["R"], case["A"])):
+            row = slice(r * L_c, (r + 1) * L_c)
+            place = (s["frame0"][c] + (n / hw).floor(), (n / case["grid_w"]).floor() % case["grid_h"], n % case["grid_w"])
+            turn = torch.cat([p[:, None] * THETA ** (-torch.arange(0, m, 2, dtype=torch.float64, device=DEV) / m)
+                              for p, m in zip(place, axis_dims(d))], 1)
+            turn = torch.polar(torch.ones_like(turn), turn)[:, None]
+            for x, w, put in ((q[row], s["wq"], out[row]), (k[row], s["wk"], kc[:, s["off"][c]:s["off"][c] + L_c].transpose(0, 1))):
+                y = x / (x.square().mean(-1, keepdim=True) + EPS).sqrt() * w.double()
+                if case["pairing"] == "halves":
+                    z = torch.complex(y[..., :d // 2].contiguous(), y[..., d // 2:].contiguous()) * turn
+                    put[..., :d // 2], put[..., d // 2:] = z.real, z.imag
+                else:
+                    put.copy_(torch.view_as_real(torch.view_as_complex(y.reshape(*y.shape[:2], -1, 2)) * turn).flatten(-2))
+            vc[:, s["off"][c]:s["off"][c] + L_c] = v[row].transpose(0, 1)
+        return {"q": out, "k": kc, "v": vc}
+    if case["kind"] == "pack":
+        levels = torch.tensor([0, .5, 1, 1.5, 2, 3, 4, 6], dtype=torch.float64, device=DEV)
+        edges = (levels[1:] + levels[:-1]) / 2
+        out = []
+        for x in (s["k_cache"], s["v_cache"]):
+            x = x[:, :case["count"]] if s["kept"] is None else torch.stack([x[h][s["kept"][h].long()] for h in range(case["H"])])
+            x = x.double().reshape(-1, 32)
+            top = x.abs().amax(1, keepdim=True)
+            power = torch.exp2(torch.floor(torch.log2(top)))
+            power = torch.where(power > top, power / 2, torch.where(2 * power <= top, 2 * power, power))
+            scale = torch.where(top >= 1.75 * power, power / 2, power / 4)
+            a = x.abs() / scale
+            i = torch.bucketize(a, edges)                  # at an edge: the level below it
+            i = i + ((i < 7) & (i % 2 == 1) & (a == edges[i.clamp(max=6)]))     # there the even one of the two
+            out.append((torch.sign(x) * levels[i] * scale).view(case["H"], case["count"], d))
+        return {"k": out[0], "v": out[1]}
+    if case["kind"] == "unpack":
+        return {"k": _doubles(s["k4"], case, case["H"], case["L"])[:, :case["count"]],
+                "v": _doubles(s["v4"], case, case["H"], case["L"])[:, :case["count"]]}
+    A, R, L_c, L, H_q, H_k = (case[k] for k in ("A", "R", "L_c", "L_clean", "H_q", "H_k"))
+    k4, v4 = _doubles(s["k4"], case, H_k, L), _doubles(s["v4"], case, H_k, L)
+    out = torch.zeros(A * L_c, H_q, d, dtype=torch.float64, device=DEV)
+    for r, c in enumerate(range(A - R, A)):
+        for h in range(H_q):
+            hk = h // (H_q // H_k)
+            k, v = ([x4[hk]] + [x[hk, o:o + L_c].double() for o in s["off"][:c + 1]]
+                    for x4, x in ((k4, s["k_cache"]), (v4, s["v_cache"])))
+            p = s["q"][r * L_c:(r + 1) * L_c, h].double() @ torch.cat(k).t().contiguous() / math.sqrt(d)
+            p = (p - p.amax(1, keepdim=True)).exp_()
+            out[r * L_c:(r + 1) * L_c, h] = p @ torch.cat(v) / p.sum(1, keepdim=True)
+    return out
+
+
+def _doubles(packed, case, H, n):
+    """A 4-bit buffer's values: sign, two bits of exponent, one of fraction (the lowest exponent without its leading one)."""
+    d = case["d"]
+    b = packed[:H * n * d // 2].view(H, n, d // 2).long()
+    c = torch.stack((b % 16, b // 16), -1).view(H, n, d // 32, 32)
+    power, half = c % 8 // 2, (c % 2).double() / 2
+    x = torch.where(power == 0, half, (1 + half) * 2.0 ** (power - 1).double())
+    x = torch.where(c >= 8, -x, x) * 2.0 ** (packed[H * n * d // 2:].view(H, n, d // 32, 1).double() - 127)
+    return x.view(H, n, d)
