@@ -28,6 +28,15 @@
  *   flowcache_kv_compact      the two halves of flowcache_kv_compress as calls of their own.
  *   flowcache_kv_compress_grouped  the same at frame / chunk key granularity (App. D.2.1).
  *
+ * and two groups of operators beside it:
+ *
+ *   flowcache_qk_norm_rope    norm of every query and key head and its rotation by (time, height,
+ *                             width), from a projection's rows into the attention's query rows and
+ *                             the K/V slots: what lies between the projections and flowcache_attend.
+ *   flowcache_kv4_pack,
+ *   flowcache_kv4_unpack      K/V rows to 4 bits and back.
+ *   flowcache_attend_kv4      flowcache_attend on a clean region that is held in 4 bits.
+ *
  * Conventions common to all calls
  * -------------------------------
  *  - Pointers marked [dev] are DEVICE pointers owned by the caller; [host] are host
@@ -349,6 +358,106 @@ size_t flowcache_kv_compress_grouped_workspace(int H_k, int L_k, int d, int budg
  */
 size_t flowcache_kv_compress_status_offset(int H_k, int L_k, int d, int budget, int group,
                                            fc_dtype dtype);
+
+/*
+ * Norm of every query and key head and its rotation by several position axes, in one pass:
+ *
+ *   y = x * (mean_e x_e^2 + norm_eps)^-1/2 * weight     over the d elements of a head (norm != 0)
+ *   (y_a, y_b) <- (y_a cos t - y_b sin t, y_a sin t + y_b cos t)     for every pair (a, b) of elements
+ *
+ * Token n (0 <= n < L_c) of active chunk c lies at time frame0[c] + n / (grid_h * grid_w), height
+ * (n / grid_w) mod grid_h and width n mod grid_w: frames of grid_h x grid_w tokens, row by row.  A chunk
+ * may end inside a frame.  The head's d / 2 pairs are dealt to the axes in that order: the first
+ * dims[0] / 2 turn with time, the next dims[1] / 2 with height, the next dims[2] / 2 with width, and
+ * what is left does not turn.  Pair i of an axis turns by  position * theta^(-2 i / dims[axis]).
+ * Elements are widened to float32, worked on in float32 (angles in float64) and rounded once.
+ *
+ *   q        [dev] rows of H_q heads of d elements (a head's elements and a row's heads follow each
+ *                  other); row block r (L_c rows) <-> chunk recompute_idx[r]; row to row q_tok_stride
+ *   k, v     [dev] the same with H_k heads and kv_new_tok_stride.  So all three may be parts of one
+ *                  fused projection's rows.  v may be NULL: then V is not written
+ *   q_weight,
+ *   k_weight [dev] [d] float32, NULL = ones (read only if norm != 0)
+ *   dims     [host] [3] even, >= 0, their sum <= d;   frame0 [host] [A]
+ *   pairing  FC_ROPE_INTERLEAVED: pair p is elements (2 p, 2 p + 1);  FC_ROPE_HALVES: (p, d / 2 + p)
+ *   q_out    [dev] [A*L_c, H_q, d] compact, as flowcache_attend takes it; may be q where q's rows follow
+ *                  each other without a gap.  Only row blocks r < *n_recompute are written
+ *   k_cache,
+ *   v_cache, active_off, recompute_idx, n_recompute   as in flowcache_attend: row block r's keys and
+ *                  values go to slot active_off[recompute_idx[r]]; nothing else in the caches is touched
+ * flowcache_attend follows with k_new = v_new = NULL.  q, k and v must not overlap what is written
+ * (but for q_out = q).
+ * Errors: null pointers, grid_h or grid_w < 1, theta <= 0 or not finite, norm_eps < 0 or not finite,
+ * dims odd, negative or beyond d, slots outside the cache or overlapping -> FC_INVALID_ARGUMENT; d not in
+ * {64, 128}, strides or pointers that are not multiples of 16 bytes -> FC_UNSUPPORTED.
+ */
+typedef enum { FC_ROPE_INTERLEAVED = 0, FC_ROPE_HALVES = 1 } fc_rope_pairing;
+int flowcache_qk_norm_rope(const void* q, int64_t q_tok_stride, const void* k, const void* v,
+                           int64_t kv_new_tok_stride, fc_dtype dtype, int H_q, int H_k, int d,
+                           int norm, float norm_eps, const float* q_weight, const float* k_weight,
+                           const int32_t* dims, fc_rope_pairing pairing, double theta, int grid_h,
+                           int grid_w, const int32_t* frame0, int L_c, int L_clean, int A,
+                           const int32_t* active_off, const int32_t* recompute_idx,
+                           const int32_t* n_recompute, void* q_out, void* k_cache, void* v_cache,
+                           int64_t kv_head_stride, int64_t kv_tok_stride, int capacity,
+                           fc_stream stream);
+
+/*
+ * K/V rows in 4 bits.  32 neighbouring elements of a row share a scale 2^(b - 127), and each is a sign
+ * and one of 0, 1/2, 1, 3/2, 2, 3, 4, 6 times it: (H_k * capacity4) * (d / 2 + d / 32) bytes for one of
+ * K and V, 0.27 of bf16.  Such a buffer holds
+ *     codes   [H_k, capacity4, d / 2]   two a byte, the even element in the low half; bit 3 the sign, bits
+ *                                       0-2 the index into the eight magnitudes
+ *     scales  [H_k, capacity4, d / 32]  the bytes b (255: the 32 elements are not numbers)
+ * Every value is exact in float32, and in bfloat16.
+ *
+ * flowcache_kv4_pack turns `count` rows of every head into 4 bits, at positions pos4 .. of the buffers:
+ * those at cache_pos .., or, with kept_idx, rows kept_idx[h][0 .. count) of head h (as written by
+ * flowcache_kv_select, so that a selection is packed without compacting the cache first).  The scale is
+ * a quarter of the largest power of two not above the block's largest magnitude, half of it from 1.75
+ * times that power on; at least 2^-126 and at most 2^125.  Values go to the nearest magnitude, halfway
+ * ones to the even index, larger ones to 6.  A block with an infinity or a NaN becomes 32 NaN.  Packing
+ * what flowcache_kv4_unpack gave reproduces the codes' values: a row that is packed again and again
+ * does not drift.  flowcache_kv4_unpack writes the values that rows pos4 .. stand for to rows cache_pos ..
+ *
+ *   k4, v4   [dev] flowcache_kv4_bytes(H_k, capacity4, d) bytes each, 16-byte aligned.  v4 and v_cache
+ *                  may both be NULL: K alone
+ *   kept_idx [dev] [H_k, count] int32 or NULL.  An entry outside [0, capacity) is skipped: its 4-bit row
+ *                  stays as it was
+ *   k_cache, v_cache, strides, capacity    as in flowcache_attend
+ * count = 0 does nothing.  Errors: rows outside [0, capacity) or [0, capacity4), null pointers ->
+ * FC_INVALID_ARGUMENT; d not in {64, 128}, misaligned pointers or strides -> FC_UNSUPPORTED.
+ * flowcache_kv4_bytes gives 0 for invalid arguments.
+ */
+size_t flowcache_kv4_bytes(int H_k, int capacity4, int d);
+int flowcache_kv4_pack(const void* k_cache, const void* v_cache, int64_t kv_head_stride,
+                       int64_t kv_tok_stride, int capacity, fc_dtype dtype, int H_k, int d,
+                       int cache_pos, const int32_t* kept_idx, int count, void* k4, void* v4,
+                       int capacity4, int pos4, fc_stream stream);
+int flowcache_kv4_unpack(const void* k4, const void* v4, int capacity4, int pos4, int count,
+                         void* k_cache, void* v_cache, int64_t kv_head_stride, int64_t kv_tok_stride,
+                         int capacity, fc_dtype dtype, int H_k, int d, int cache_pos,
+                         fc_stream stream);
+
+/*
+ * flowcache_attend with the clean region in 4 bits: a query of active chunk c sees rows [0, L_clean) of
+ * k4 / v4 (as above, written by flowcache_kv4_pack) and the slots of active chunks 0..c, which alone lie
+ * in k_cache / v_cache: active_off may start at 0.  Arguments, errors and workspace as there, and
+ *
+ *   k4, v4   [dev] buffers of capacity4 rows per head; may be NULL if L_clean = 0
+ *   dtype    FC_BF16 (type of q, the caches and out); FC_F32 -> FC_UNSUPPORTED.  The 4-bit values are
+ *            bf16 operands without rounding, so the result is flowcache_attend's on the unpacked rows
+ * The importance mass is not emitted here: at a commit the clean keys are unpacked for the selection
+ * anyway, and flowcache_attention_mass takes them from there.
+ */
+int flowcache_attend_kv4(const void* q, const void* k_new, const void* v_new, const void* k4,
+                         const void* v4, int capacity4, void* k_cache, void* v_cache,
+                         int64_t kv_head_stride, int64_t kv_tok_stride, int capacity, fc_dtype dtype,
+                         int H_q, int H_k, int d, int L_c, int L_clean, int A,
+                         const int32_t* active_off, const int32_t* recompute_idx,
+                         const int32_t* n_recompute, float softmax_scale, void* out, float* lse,
+                         void* workspace, size_t workspace_bytes, fc_stream stream);
+size_t flowcache_attend_kv4_workspace(int A, int L_c, int H_q, int d);
 
 #ifdef __cplusplus
 }

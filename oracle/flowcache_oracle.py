@@ -24,6 +24,8 @@ special cases) live in ``tests/test_oracle_*.py``.  Pin status:
   kv_compress_grouped ...................... pinned (group = 1 is kv_compress; identical tokens
                                              inside each group reduce it to kv_compress on one
                                              token per group; hand-worked case; means stay float64)
+  norm_heads, rotate, token_positions ...... pinned (complex arithmetic, invariants of rotations)
+  kv4_pack, kv4_values ..................... pinned (brute-force nearest magnitude, every code)
   Parity unpinned (the paper gives no value): the max-pool kernel size, the exact
   attention mask and the order of the surviving tokens rest on the readings below.
 
@@ -449,3 +451,75 @@ def kv_compress_grouped(k_cache: np.ndarray, v_cache: np.ndarray, L_k: int, budg
         v_new[h, :budget] = v_cache[h, kept[h]]
         scores.append(sc)
     return kept, k_new, v_new, scores
+
+
+# ======================================================================================
+# Between the projections and the attention; rows in 4 bits
+# ======================================================================================
+def token_positions(frame0: int, L_c: int, grid_h: int, grid_w: int) -> np.ndarray:
+    """(time, height, width) of a chunk's tokens ``[L_c, 3]``: frames of grid_h x grid_w tokens, row by row."""
+    out = np.zeros((L_c, 3), dtype=np.int64)
+    for n in range(L_c):
+        out[n] = (frame0 + n // (grid_h * grid_w), (n // grid_w) % grid_h, n % grid_w)
+    return out
+
+
+def norm_heads(x: np.ndarray, weight: Optional[np.ndarray], eps: float) -> np.ndarray:
+    """x ``[rows, H, d]`` over the root mean square of each head's d elements, times ``weight [d]``."""
+    x = widen(x)
+    y = x / np.sqrt((x * x).mean(axis=-1, keepdims=True) + eps)
+    return y if weight is None else y * widen(weight)
+
+
+def rotate(x: np.ndarray, pos: np.ndarray, dims: Sequence[int], theta: float, halves: bool) -> np.ndarray:
+    """x ``[rows, H, d]``: pair after pair of every head turned by its axis' position (``pos [rows, 3]``) times
+    theta^(-2 i / dims[axis]); the first dims[0] / 2 pairs belong to time, then height, then width."""
+    x = widen(x)
+    d = x.shape[-1]
+    y = x.copy()
+    p = 0
+    for axis in range(3):
+        for i in range(dims[axis] // 2):
+            angle = pos[:, axis].astype(np.float64) * theta ** (-2.0 * i / dims[axis])
+            c, s = np.cos(angle)[:, None], np.sin(angle)[:, None]
+            a, b = (p, d // 2 + p) if halves else (2 * p, 2 * p + 1)
+            y[..., a] = x[..., a] * c - x[..., b] * s
+            y[..., b] = x[..., a] * s + x[..., b] * c
+            p += 1
+    return y
+
+
+KV4_MAGNITUDES = (0.0, 0.5, 1.0, 1.5, 2.0, 3.0, 4.0, 6.0)
+
+
+def kv4_pack(x: np.ndarray) -> Tuple[np.ndarray, np.ndarray]:
+    """Rows ``[H, n, d]`` -> (codes ``[H, n, d / 2]``, scales ``[H, n, d / 32]``), both uint8.  A block's scale is a quarter
+    of the largest power of two not above its largest magnitude, half of it from 1.75 times that power on, within
+    [2^-126, 2^125]; nearest magnitude, halfway to the even index."""
+    x = widen(x)
+    H, n, d = x.shape
+    b = x.reshape(H, n, d // 32, 32)
+    top = np.abs(b).max(axis=-1)
+    ok = np.isfinite(top)
+    frac, exp = np.frexp(np.where(ok, top, 0.0))              # top = frac * 2^exp, frac in [1/2, 1)
+    e = np.where(top == 0, -126, exp - 3 + (frac >= 0.875))
+    e = np.clip(e, -126, 125)
+    a = np.where(ok[..., None], b, 0.0) / np.exp2(e.astype(np.float64))[..., None]
+    mag = np.array(KV4_MAGNITUDES)
+    dist = np.abs(np.abs(a)[..., None] - mag)
+    best = dist.min(axis=-1, keepdims=True)
+    code = np.argmax(dist == best, axis=-1)                   # the lower of two equally near ones
+    tie = (dist == best).sum(axis=-1) == 2
+    code = np.where(tie & (code % 2 == 1), code + 1, code)
+    code = code + 8 * (np.signbit(a) & ok[..., None])
+    code = code.reshape(H, n, d // 2, 2).astype(np.uint8)
+    return code[..., 0] | (code[..., 1] << 4), np.where(ok, e + 127, 255).astype(np.uint8)
+
+
+def kv4_values(codes: np.ndarray, scales: np.ndarray) -> np.ndarray:
+    """What codes and scales stand for, ``[H, n, d]`` float64."""
+    H, n, half = codes.shape
+    c = np.stack([codes & 15, codes >> 4], axis=-1).reshape(H, n, -1, 32)
+    v = np.array(KV4_MAGNITUDES + tuple(-m for m in KV4_MAGNITUDES))[c]
+    s = np.where(scales == 255, np.nan, np.exp2(scales.astype(np.float64) - 127))
+    return (v * s[..., None]).reshape(H, n, 2 * half)

@@ -33,6 +33,8 @@ EXPORTS = (
     "flowcache_kv_select", "flowcache_kv_compact",
     "flowcache_kv_compress_grouped", "flowcache_kv_compress_grouped_workspace",
     "flowcache_kv_compress_status_offset",
+    "flowcache_qk_norm_rope", "flowcache_kv4_bytes", "flowcache_kv4_pack", "flowcache_kv4_unpack",
+    "flowcache_attend_kv4", "flowcache_attend_kv4_workspace",
     "flowcache_sched_state_bytes", "flowcache_sched_init", "flowcache_sched_capacity",
     "flowcache_sched_total_ticks", "flowcache_sched_next",
 )
@@ -106,6 +108,24 @@ def lib() -> ctypes.CDLL:
                                                 c_int, c_vp, c_int, c_d, c_vp, c_vp, c_sz, c_vp]
     L.flowcache_kv_compress_status_offset.restype = c_sz
     L.flowcache_kv_compress_status_offset.argtypes = [c_int] * 6
+    L.flowcache_qk_norm_rope.restype = c_int
+    L.flowcache_qk_norm_rope.argtypes = [c_vp, c_i64, c_vp, c_vp, c_i64, c_int, c_int, c_int, c_int, c_int, c_f,
+                                         c_vp, c_vp, c_vp, c_int, c_d, c_int, c_int, c_vp, c_int, c_int, c_int,
+                                         c_vp, c_vp, c_vp, c_vp, c_vp, c_vp, c_i64, c_i64, c_int, c_vp]
+    L.flowcache_kv4_bytes.restype = c_sz
+    L.flowcache_kv4_bytes.argtypes = [c_int, c_int, c_int]
+    L.flowcache_kv4_pack.restype = c_int
+    L.flowcache_kv4_pack.argtypes = [c_vp, c_vp, c_i64, c_i64, c_int, c_int, c_int, c_int, c_int, c_vp, c_int,
+                                     c_vp, c_vp, c_int, c_int, c_vp]
+    L.flowcache_kv4_unpack.restype = c_int
+    L.flowcache_kv4_unpack.argtypes = [c_vp, c_vp, c_int, c_int, c_int, c_vp, c_vp, c_i64, c_i64, c_int, c_int,
+                                       c_int, c_int, c_int, c_vp]
+    L.flowcache_attend_kv4_workspace.restype = c_sz
+    L.flowcache_attend_kv4_workspace.argtypes = [c_int] * 4
+    L.flowcache_attend_kv4.restype = c_int
+    L.flowcache_attend_kv4.argtypes = [c_vp, c_vp, c_vp, c_vp, c_vp, c_int, c_vp, c_vp, c_i64, c_i64, c_int, c_int,
+                                       c_int, c_int, c_int, c_int, c_int, c_int, c_vp, c_vp, c_vp, c_f, c_vp, c_vp,
+                                       c_vp, c_sz, c_vp]
     L.flowcache_sched_state_bytes.restype = c_sz
     L.flowcache_sched_state_bytes.argtypes = []
     L.flowcache_sched_init.restype = c_int
@@ -422,6 +442,173 @@ def flowcache_kv_compress_grouped(k_cache: torch.Tensor, v_cache: torch.Tensor, 
     if check_status:
         _raise_on_compaction_status("flowcache_kv_compress_grouped", workspace, H_k, L_k, d, budget, code, group)
     return kept_idx
+
+
+# ---- between the projections and the attention; a clean region in 4 bits ---------------------
+def _empty(shape, dtype, device, stream=None) -> torch.Tensor:
+    """An output of a call, allocated (as its scratch is) for the stream that writes it."""
+    if isinstance(stream, torch.cuda.Stream):
+        with torch.cuda.stream(stream):
+            return torch.empty(shape, dtype=dtype, device=device)
+    return torch.empty(shape, dtype=dtype, device=device)
+
+
+def _same_device(call: str, stream, first: torch.Tensor, *others: Optional[torch.Tensor]) -> None:
+    """A kernel runs on the stream's device, by default the current one: tensors of another are refused."""
+    dev = first.device
+    for t in others:
+        if t is not None and t.device != dev:
+            raise ValueError(f"{call}: tensors on {dev} and {t.device}")
+    if dev.type != "cuda":
+        raise ValueError(f"{call}: tensors on {dev}, not on a GPU")
+    on = torch._C._cuda_getDevice() if stream is None else stream.device_index
+    if dev.index != on:
+        raise ValueError(f"{call}: tensors on {dev}, the stream on device {on}")
+
+
+_PAIRINGS = {"interleaved": 0, "halves": 1}
+
+
+def _heads_of_rows(call: str, name: str, x: torch.Tensor, rows: int, d: int, dtype) -> int:
+    """Elements from row to row of ``[rows, H, d]``, whose heads and elements follow each other."""
+    if x.dim() != 3 or x.shape[0] != rows or x.shape[2] != d or x.dtype != dtype:
+        raise ValueError(f"{call}: {name} is [{rows}, heads, {d}] of {dtype}, got {tuple(x.shape)} of {x.dtype}")
+    if x.stride(2) != 1 or (x.shape[1] > 1 and x.stride(1) != d):
+        raise ValueError(f"{call}: the heads of a row of {name} have to follow each other, got strides {x.stride()}")
+    return x.stride(0) if rows > 1 else max(x.stride(0), x.shape[1] * d)
+
+
+def flowcache_qk_norm_rope(q: torch.Tensor, k: torch.Tensor, v: Optional[torch.Tensor], k_cache: torch.Tensor,
+                           v_cache: Optional[torch.Tensor], L_c: int, L_clean: int, active_off: Sequence[int],
+                           recompute_idx: torch.Tensor, n_recompute: torch.Tensor, dims: Sequence[int],
+                           grid: Sequence[int], frame0: Sequence[int], theta: float = 10000.0,
+                           pairing: str = "interleaved", q_weight: Optional[torch.Tensor] = None,
+                           k_weight: Optional[torch.Tensor] = None, norm_eps: Optional[float] = 1e-6,
+                           q_out: Optional[torch.Tensor] = None, stream=None) -> torch.Tensor:
+    """Per-head RMS norm of queries and keys (``norm_eps=None``: none) and their rotation by (time, height,
+    width), in one pass.  q ``[A*L_c, H_q, d]``, k and v ``[A*L_c, H_k, d]`` may be parts of one fused projection's
+    rows.  Keys and values go to the recompute chunks' slots of the caches ``[H_k, capacity, d]``; the queries are
+    returned ``[A*L_c, H_q, d]``, ready for ``flowcache_attend(q, None, None, ...)``.
+
+    ``dims``: how many of a head's elements turn with time, height and width; ``grid``: (height, width) of a
+    frame in tokens; ``frame0``: the first frame of each active chunk; weights: float32 ``[d]``."""
+    call = "flowcache_qk_norm_rope"
+    H_k, capacity, d = k_cache.shape
+    A, H_q, rows = len(active_off), q.shape[1], q.shape[0]
+    if rows != A * L_c or len(dims) != 3 or len(grid) != 2 or len(frame0) != A:
+        raise ValueError(f"{call}: q has A * L_c rows, dims three numbers, grid two, frame0 one per active chunk")
+    if pairing not in _PAIRINGS:
+        raise ValueError(f"{call}: pairing is one of {sorted(_PAIRINGS)}, got {pairing!r}")
+    _same_device(call, stream, q, k, v, k_cache, v_cache, recompute_idx, n_recompute, q_weight, k_weight, q_out)
+    qs = _heads_of_rows(call, "q", q, rows, d, k_cache.dtype)
+    ks = _heads_of_rows(call, "k", k, rows, d, k_cache.dtype)
+    assert k.shape[1] == H_k and k_cache.stride(2) == 1 and (v is None) == (v_cache is None)
+    if v is not None:
+        if _heads_of_rows(call, "v", v, rows, d, k_cache.dtype) != ks or v.shape[1] != H_k:
+            raise ValueError(f"{call}: k and v have the same heads and row stride")
+        assert v_cache.stride() == k_cache.stride() and v_cache.shape == k_cache.shape and v_cache.dtype == k_cache.dtype
+    for w in (q_weight, k_weight):
+        if w is not None and (w.dtype != torch.float32 or tuple(w.shape) != (d,) or not w.is_contiguous()):
+            raise ValueError(f"{call}: weights are float32 [{d}]")
+    if q_out is None:
+        q_out = _empty((rows, H_q, d), q.dtype, q.device, stream)
+    assert q_out.shape == (rows, H_q, d) and q_out.is_contiguous() and q_out.dtype == q.dtype
+    i32 = ctypes.c_int32
+    st = (_lib or lib()).flowcache_qk_norm_rope(
+        _ptr(q), qs, _ptr(k), _ptr(v), ks, _dtype_code(k_cache), H_q, H_k, d, int(norm_eps is not None),
+        0.0 if norm_eps is None else float(norm_eps), _ptr(q_weight), _ptr(k_weight),
+        (i32 * 3)(*[int(x) for x in dims]), _PAIRINGS[pairing], float(theta), int(grid[0]), int(grid[1]),
+        (i32 * A)(*[int(x) for x in frame0]), int(L_c), int(L_clean), A, (i32 * A)(*[int(x) for x in active_off]),
+        _ptr(recompute_idx), _ptr(n_recompute), _ptr(q_out), _ptr(k_cache), _ptr(v_cache), k_cache.stride(0),
+        k_cache.stride(1), capacity, _stream(stream))
+    _check(call, st)
+    return q_out
+
+
+def kv4_buffer(H_k: int, capacity4: int, d: int, device="cuda") -> torch.Tensor:
+    """A buffer for ``capacity4`` rows per head of K or V in 4 bits."""
+    nbytes = (_lib or lib()).flowcache_kv4_bytes(int(H_k), int(capacity4), int(d))
+    if nbytes == 0:
+        raise FlowCacheError("flowcache_kv4_bytes", FC_INVALID_ARGUMENT)
+    return torch.empty(nbytes, dtype=torch.uint8, device=device)
+
+
+def _kv4_shapes(call: str, stream, k4, v4, capacity4: int, k_cache, v_cache, *others) -> None:
+    H_k, _, d = k_cache.shape
+    _same_device(call, stream, k_cache, v_cache, k4, v4, *others)
+    assert k_cache.stride(2) == 1 and (v4 is None) == (v_cache is None)
+    assert v_cache is None or (v_cache.stride() == k_cache.stride() and v_cache.shape == k_cache.shape
+                               and v_cache.dtype == k_cache.dtype)
+    need = H_k * int(capacity4) * (d // 2 + d // 32)
+    for x in (k4, v4):
+        if x is not None and (x.dtype != torch.uint8 or not x.is_contiguous() or x.numel() < need):
+            raise ValueError(f"{call}: a 4-bit buffer of {capacity4} rows per head is {need} contiguous bytes of uint8")
+
+
+def flowcache_kv4_pack(k_cache: torch.Tensor, v_cache: Optional[torch.Tensor], k4: torch.Tensor,
+                       v4: Optional[torch.Tensor], capacity4: int, count: int, cache_pos: int = 0, pos4: int = 0,
+                       kept_idx: Optional[torch.Tensor] = None, stream=None) -> None:
+    """Rows ``cache_pos .. + count`` of the caches ``[H_k, capacity, d]`` (or rows ``kept_idx`` ``[H_k, count]`` of each
+    head) in 4 bits, to rows ``pos4 ..`` of the buffers."""
+    call = "flowcache_kv4_pack"
+    H_k, capacity, d = k_cache.shape
+    _kv4_shapes(call, stream, k4, v4, capacity4, k_cache, v_cache, kept_idx)
+    assert kept_idx is None or (kept_idx.dtype == torch.int32 and kept_idx.is_contiguous() and kept_idx.shape == (H_k, count))
+    st = (_lib or lib()).flowcache_kv4_pack(_ptr(k_cache), _ptr(v_cache), k_cache.stride(0), k_cache.stride(1), capacity,
+                                            _dtype_code(k_cache), H_k, d, int(cache_pos), _ptr(kept_idx), int(count),
+                                            _ptr(k4), _ptr(v4), int(capacity4), int(pos4), _stream(stream))
+    _check(call, st)
+
+
+def flowcache_kv4_unpack(k4: torch.Tensor, v4: Optional[torch.Tensor], capacity4: int, k_cache: torch.Tensor,
+                         v_cache: Optional[torch.Tensor], count: int, pos4: int = 0, cache_pos: int = 0,
+                         stream=None) -> None:
+    """What rows ``pos4 .. + count`` of the buffers stand for, to rows ``cache_pos ..`` of the caches."""
+    call = "flowcache_kv4_unpack"
+    H_k, capacity, d = k_cache.shape
+    _kv4_shapes(call, stream, k4, v4, capacity4, k_cache, v_cache)
+    st = (_lib or lib()).flowcache_kv4_unpack(_ptr(k4), _ptr(v4), int(capacity4), int(pos4), int(count), _ptr(k_cache),
+                                              _ptr(v_cache), k_cache.stride(0), k_cache.stride(1), capacity,
+                                              _dtype_code(k_cache), H_k, d, int(cache_pos), _stream(stream))
+    _check(call, st)
+
+
+def flowcache_attend_kv4(q: torch.Tensor, k_new: Optional[torch.Tensor], v_new: Optional[torch.Tensor],
+                         k4: Optional[torch.Tensor], v4: Optional[torch.Tensor], capacity4: int,
+                         k_cache: torch.Tensor, v_cache: torch.Tensor, L_c: int, L_clean: int,
+                         active_off: Sequence[int], recompute_idx: torch.Tensor, n_recompute: torch.Tensor,
+                         softmax_scale: float = 0.0, out: Optional[torch.Tensor] = None, want_lse: bool = True,
+                         workspace: Optional[torch.Tensor] = None, stream=None) -> Dict[str, Optional[torch.Tensor]]:
+    """:func:`flowcache_attend` with the clean region in the 4-bit buffers k4 / v4; the caches ``[H_k, capacity, d]``
+    (bfloat16) hold the active chunks' slots alone.  k4 and v4 may be None if ``L_clean`` is 0."""
+    call = "flowcache_attend_kv4"
+    rows, H_q, d = q.shape
+    H_k, capacity, _ = k_cache.shape
+    A = len(active_off)
+    assert q.is_contiguous() and rows == A * L_c and k_cache.shape[2] == d and (k4 is None) == (v4 is None)
+    assert q.dtype == k_cache.dtype and v_cache is not None
+    for x in (k_new, v_new):
+        assert x is None or (x.is_contiguous() and x.shape == (rows, H_k, d) and x.dtype == q.dtype)
+    if k4 is None:
+        _same_device(call, stream, q, k_cache, v_cache)
+    else:
+        _kv4_shapes(call, stream, k4, v4, capacity4, k_cache, v_cache)
+    _same_device(call, stream, q, k_cache, k_new, v_new, recompute_idx, n_recompute, out, workspace)
+    if out is None:
+        out = _empty(q.shape, q.dtype, q.device, stream)
+    assert out.is_contiguous() and out.shape == q.shape and out.dtype == q.dtype
+    lse = _empty((H_q, rows), torch.float32, q.device, stream) if want_lse else None
+    off = (ctypes.c_int32 * A)(*[int(x) for x in active_off])
+    L = _lib or lib()
+    if workspace is None:
+        workspace = _workspace(L.flowcache_attend_kv4_workspace(A, L_c, H_q, d), q.device, stream)
+    st = L.flowcache_attend_kv4(_ptr(q), _ptr(k_new), _ptr(v_new), _ptr(k4), _ptr(v4), int(capacity4), _ptr(k_cache),
+                                _ptr(v_cache), k_cache.stride(0), k_cache.stride(1), capacity, _dtype_code(q), H_q, H_k,
+                                d, int(L_c), int(L_clean), A, off, _ptr(recompute_idx), _ptr(n_recompute),
+                                float(softmax_scale), _ptr(out), _ptr(lse), _ptr(workspace), workspace.numel(),
+                                _stream(stream))
+    _check(call, st)
+    return {"out": out, "lse": lse}
 
 
 # --------------------------------------------------------------------------------------

@@ -15,7 +15,7 @@ CSRC = os.path.join(HERE, "csrc")
 OBJ = os.path.join(HERE, "_build")
 LIB = os.path.join(HERE, "libflowcache.so")
 SOURCES = ["api.hip", "decide.hip", "attend_f32.hip", "attend_bf16.hip", "mass.hip",
-           "compress.hip", "residual.hip", "sched.cpp"]
+           "compress.hip", "residual.hip", "rope.hip", "kv4.hip", "sched.cpp"]
 HIPCC = os.environ.get("HIPCC", "/opt/rocm/bin/hipcc")
 FLAGS = ["--offload-arch=gfx950", "-O3", "-std=c++17", "-fPIC", "-fvisibility=hidden",
          "-Xclang", "-target-feature", "-Xclang", "-packed-fp32-ops",

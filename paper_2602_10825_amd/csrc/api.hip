@@ -249,7 +249,7 @@ int flowcache_attend(const void* q, const void* k_new, const void* v_new, void* 
     std::memcpy(at.active_off, active_off, sizeof(int32_t) * A);
     at.rec_idx = recompute_idx; at.n_rec = n_recompute; at.scale = scale;
     at.ws = workspace; at.ws_bytes = workspace ? workspace_bytes : 0;
-    st = (dtype == FC_BF16) ? fc_launch_attend_bf16(at, s) : fc_launch_attend_f32(at, s);
+    st = (dtype == FC_BF16) ? fc_launch_attend_bf16(at, nullptr, s) : fc_launch_attend_f32(at, s);
     if (st != FC_OK) return st;
 
     if (mass) {
@@ -263,6 +263,146 @@ int flowcache_attend(const void* q, const void* k_new, const void* v_new, void* 
         if (st != FC_OK) return st;
     }
     return FC_OK;
+}
+
+// ------------------------------------------------------------------ qk_norm_rope
+int flowcache_qk_norm_rope(const void* q, int64_t q_tok_stride, const void* k, const void* v,
+                           int64_t kv_new_tok_stride, fc_dtype dtype, int H_q, int H_k, int d,
+                           int norm, float norm_eps, const float* q_weight, const float* k_weight,
+                           const int32_t* dims, fc_rope_pairing pairing, double theta, int grid_h,
+                           int grid_w, const int32_t* frame0, int L_c, int L_clean, int A,
+                           const int32_t* active_off, const int32_t* recompute_idx,
+                           const int32_t* n_recompute, void* q_out, void* k_cache, void* v_cache,
+                           int64_t kv_head_stride, int64_t kv_tok_stride, int capacity,
+                           fc_stream stream) {
+    if (!q || !k || !dims || !frame0 || !active_off || !recompute_idx || !n_recompute || !q_out)
+        return FC_INVALID_ARGUMENT;
+    if (A < 1 || A > FC_MAX_ACTIVE || L_c < 1 || L_clean < 0 || H_q < 1 || capacity < 1)
+        return FC_INVALID_ARGUMENT;
+    int st = check_kv_layout(k_cache, v ? v_cache : k_cache, kv_head_stride, kv_tok_stride, capacity, dtype, H_k, d);
+    if (st != FC_OK) return st;
+    st = check_slots(A, L_c, L_clean, capacity, active_off);
+    if (st != FC_OK) return st;
+    if (grid_h < 1 || grid_w < 1 || !(theta > 0.0) || !std::isfinite(theta)) return FC_INVALID_ARGUMENT;
+    if (norm && (!(norm_eps >= 0.f) || !std::isfinite(norm_eps))) return FC_INVALID_ARGUMENT;
+    if (pairing != FC_ROPE_INTERLEAVED && pairing != FC_ROPE_HALVES) return FC_INVALID_ARGUMENT;
+    int64_t sum = 0;
+    for (int i = 0; i < 3; ++i) {
+        if (dims[i] < 0 || dims[i] % 2 != 0) return FC_INVALID_ARGUMENT;
+        sum += dims[i];
+    }
+    if (sum > d) return FC_INVALID_ARGUMENT;
+    const int per16 = 16 / esize(dtype);
+    if (q_tok_stride < (int64_t)H_q * d || kv_new_tok_stride < (int64_t)H_k * d) return FC_INVALID_ARGUMENT;
+    if (q_tok_stride % per16 != 0 || kv_new_tok_stride % per16 != 0) return FC_UNSUPPORTED;
+    if (!aligned16(q) || !aligned16(k) || !aligned16(v) || !aligned16(q_out)) return FC_UNSUPPORTED;
+    if ((int64_t)A * L_c > INT32_MAX || (int64_t)grid_h * grid_w > INT32_MAX) return FC_UNSUPPORTED;
+
+    FcRopeArgs a{};
+    a.q = q; a.k = k; a.v = v; a.q_stride = q_tok_stride; a.kv_stride = kv_new_tok_stride;
+    a.q_out = q_out; a.k_cache = k_cache; a.v_cache = v_cache;
+    a.head_stride = kv_head_stride; a.tok_stride = kv_tok_stride;
+    a.dtype = dtype; a.H_q = H_q; a.H_k = H_k; a.d = d; a.L_c = L_c; a.A = A;
+    a.q_weight = q_weight; a.k_weight = k_weight; a.eps = norm_eps; a.norm = norm; a.pairing = pairing;
+    a.grid_h = grid_h; a.grid_w = grid_w;
+    a.pairs_t = dims[0] / 2; a.pairs_th = (dims[0] + dims[1]) / 2;
+    for (int axis = 0, p = 0; axis < 3; ++axis)
+        for (int i = 0; i < dims[axis] / 2; ++i)
+            a.turns[p++] = std::pow(theta, -2.0 * i / dims[axis]) / (2.0 * M_PI);
+    std::memcpy(a.frame0, frame0, sizeof(int32_t) * A);
+    std::memcpy(a.active_off, active_off, sizeof(int32_t) * A);
+    a.rec_idx = recompute_idx; a.n_rec = n_recompute;
+    return fc_launch_qk_norm_rope(a, (hipStream_t)stream);
+}
+
+// ------------------------------------------------------------------ kv4
+size_t flowcache_kv4_bytes(int H_k, int capacity4, int d) {
+    if (H_k < 1 || capacity4 < 1 || (d != 64 && d != 128)) return 0;
+    return (size_t)H_k * capacity4 * (d / 2 + d / 32);
+}
+
+namespace {
+bool rows_inside(int pos, int count, int capacity) { return pos >= 0 && count >= 0 && (int64_t)pos + count <= capacity; }
+
+int check_kv4(const FcKv4Args& a, int capacity) {
+    if (!a.k4 || (a.v4 == nullptr) != (a.v_cache == nullptr)) return FC_INVALID_ARGUMENT;
+    if (a.capacity4 < 1 || capacity < 1 || !rows_inside(a.pos4, a.count, (int)a.capacity4)) return FC_INVALID_ARGUMENT;
+    if (a.kept ? a.cache_pos != 0 : !rows_inside(a.cache_pos, a.count, capacity)) return FC_INVALID_ARGUMENT;
+    const int st = check_kv_layout(a.k_cache, a.v_cache ? a.v_cache : a.k_cache, a.head_stride, a.tok_stride, capacity, a.dtype, a.H_k, a.d);
+    if (st != FC_OK) return st;
+    // (heads are a dimension of the launch's grid)
+    return aligned16(a.k4) && aligned16(a.v4) && a.H_k <= 65535 ? FC_OK : FC_UNSUPPORTED;
+}
+}  // namespace
+
+int flowcache_kv4_pack(const void* k_cache, const void* v_cache, int64_t kv_head_stride,
+                       int64_t kv_tok_stride, int capacity, fc_dtype dtype, int H_k, int d,
+                       int cache_pos, const int32_t* kept_idx, int count, void* k4, void* v4,
+                       int capacity4, int pos4, fc_stream stream) {
+    // (packing only reads the caches)
+    FcKv4Args a{const_cast<void*>(k_cache), const_cast<void*>(v_cache), kv_head_stride, kv_tok_stride, dtype, H_k, d, capacity,
+                (uint8_t*)k4, (uint8_t*)v4, capacity4, cache_pos, pos4, count, kept_idx};
+    const int st = check_kv4(a, capacity);
+    return st != FC_OK ? st : fc_launch_kv4_pack(a, (hipStream_t)stream);
+}
+
+int flowcache_kv4_unpack(const void* k4, const void* v4, int capacity4, int pos4, int count,
+                         void* k_cache, void* v_cache, int64_t kv_head_stride, int64_t kv_tok_stride,
+                         int capacity, fc_dtype dtype, int H_k, int d, int cache_pos,
+                         fc_stream stream) {
+    // (unpacking only reads the 4-bit buffers)
+    FcKv4Args a{k_cache, v_cache, kv_head_stride, kv_tok_stride, dtype, H_k, d, capacity,
+                (uint8_t*)const_cast<void*>(k4), (uint8_t*)const_cast<void*>(v4), capacity4, cache_pos, pos4, count, nullptr};
+    const int st = check_kv4(a, capacity);
+    return st != FC_OK ? st : fc_launch_kv4_unpack(a, (hipStream_t)stream);
+}
+
+size_t flowcache_attend_kv4_workspace(int A, int L_c, int H_q, int d) {
+    if (A < 1 || A > FC_MAX_ACTIVE || L_c < 1 || H_q < 1 || (d != 64 && d != 128)) return 0;
+    return 256 + fc_attend_split_workspace(A, L_c, H_q, d);
+}
+
+int flowcache_attend_kv4(const void* q, const void* k_new, const void* v_new, const void* k4,
+                         const void* v4, int capacity4, void* k_cache, void* v_cache,
+                         int64_t kv_head_stride, int64_t kv_tok_stride, int capacity, fc_dtype dtype,
+                         int H_q, int H_k, int d, int L_c, int L_clean, int A,
+                         const int32_t* active_off, const int32_t* recompute_idx,
+                         const int32_t* n_recompute, float softmax_scale, void* out, float* lse,
+                         void* workspace, size_t workspace_bytes, fc_stream stream) {
+    if (!q || !out || !active_off || !recompute_idx || !n_recompute) return FC_INVALID_ARGUMENT;
+    if ((k_new == nullptr) != (v_new == nullptr)) return FC_INVALID_ARGUMENT;
+    if (A < 1 || A > FC_MAX_ACTIVE || L_c < 1 || L_clean < 0 || H_q < 1 || capacity < 1)
+        return FC_INVALID_ARGUMENT;
+    if (L_clean > 0 && (!k4 || !v4 || capacity4 < L_clean)) return FC_INVALID_ARGUMENT;
+    int st = check_kv_layout(k_cache, v_cache, kv_head_stride, kv_tok_stride, capacity, dtype, H_k, d);
+    if (st != FC_OK) return st;
+    if (H_q % H_k != 0) return FC_INVALID_ARGUMENT;
+    if (!(softmax_scale >= 0.f) || !std::isfinite(softmax_scale)) return FC_INVALID_ARGUMENT;
+    if (dtype != FC_BF16 || (int64_t)A * L_c > INT32_MAX || (int64_t)L_clean + (int64_t)A * L_c > INT32_MAX) return FC_UNSUPPORTED;
+    st = check_slots(A, L_c, 0, capacity, active_off);
+    if (st != FC_OK) return st;
+    if (!aligned16(q) || !aligned16(out) || (k_new && (!aligned16(k_new) || !aligned16(v_new))) ||
+        (L_clean > 0 && (!aligned16(k4) || !aligned16(v4))))
+        return FC_UNSUPPORTED;
+
+    if (k_new) {
+        st = flowcache_scatter_kv(k_new, v_new, k_cache, v_cache, kv_head_stride, kv_tok_stride,
+                                  capacity, dtype, H_k, d, L_c, 0, A, active_off, recompute_idx,
+                                  n_recompute, stream);
+        if (st != FC_OK) return st;
+    }
+
+    FcAttendArgs at{};
+    at.q = q; at.out = out; at.lse = lse; at.k_cache = k_cache; at.v_cache = v_cache;
+    at.head_stride = kv_head_stride; at.tok_stride = kv_tok_stride; at.dtype = dtype;
+    at.H_q = H_q; at.H_k = H_k; at.d = d; at.L_c = L_c; at.L_clean = L_clean; at.A = A;
+    std::memcpy(at.active_off, active_off, sizeof(int32_t) * A);
+    at.rec_idx = recompute_idx; at.n_rec = n_recompute;
+    at.scale = softmax_scale > 0.f ? softmax_scale : 1.0f / std::sqrt((float)d);
+    at.ws = workspace; at.ws_bytes = workspace ? workspace_bytes : 0;
+    const int64_t rows = L_clean > 0 ? capacity4 : 0;
+    const FcKv4 clean4{(const uint8_t*)k4, (const uint8_t*)v4, rows * (d / 2), rows * (d / 32), H_k * rows * (d / 2)};
+    return fc_launch_attend_bf16(at, &clean4, (hipStream_t)stream);
 }
 
 // ------------------------------------------------------------------ kv_compress

@@ -124,7 +124,30 @@ struct FcAttendArgs {
 };
 size_t fc_attend_split_workspace(int A, int L_c, int H_q, int d);
 int fc_launch_attend_f32(const FcAttendArgs& a, hipStream_t s);
-int fc_launch_attend_bf16(const FcAttendArgs& a, hipStream_t s);
+// K or V rows in 4 bits (kv4.hpp), head by head: codes, then (from byte scales_at on) scales.
+struct FcKv4 { const uint8_t* k; const uint8_t* v; int64_t head_codes, head_scales, scales_at; };
+// clean4: the clean region in 4 bits, the caches hold the slots alone; NULL: it is the caches' first part
+int fc_launch_attend_bf16(const FcAttendArgs& a, const FcKv4* clean4, hipStream_t s);
+
+struct FcKv4Args {
+    void* k_cache; void* v_cache; int64_t head_stride, tok_stride; fc_dtype dtype; int H_k, d, L_k;
+    uint8_t* k4; uint8_t* v4; int64_t capacity4; int cache_pos, pos4, count;
+    const int32_t* kept;    // source rows of a packing, [H_k, count]; NULL: cache_pos + i
+};
+int fc_launch_kv4_pack(const FcKv4Args& a, hipStream_t s);
+int fc_launch_kv4_unpack(const FcKv4Args& a, hipStream_t s);
+
+struct FcRopeArgs {
+    const void* q; const void* k; const void* v; int64_t q_stride, kv_stride;    // elements from token to token
+    void* q_out; void* k_cache; void* v_cache; int64_t head_stride, tok_stride;
+    fc_dtype dtype; int H_q, H_k, d, L_c, A;
+    const float* q_weight; const float* k_weight; float eps; int norm, pairing;
+    int grid_h, grid_w, pairs_t, pairs_th;       // pairs [0, pairs_t) turn with time, [pairs_t, pairs_th) with height
+    double turns[64];                            // revolutions per unit of position; 0: a pair that does not turn
+    int32_t frame0[FC_MAX_ACTIVE], active_off[FC_MAX_ACTIVE];
+    const int32_t* rec_idx; const int32_t* n_rec;
+};
+int fc_launch_qk_norm_rope(const FcRopeArgs& a, hipStream_t s);
 
 struct FcScatterArgs {
     const void* k_new; const void* v_new; void* k_cache; void* v_cache;
