@@ -138,7 +138,7 @@ def _to4(x):
     a = torch.ldexp(b, -e)
     s = a.abs()
     code = ((s > .25).to(torch.uint8) + (s >= .75) + (s > 1.25) + (s >= 1.75) + (s > 2.5) + (s >= 3.5) + (s > 5.)
-            + 8 * (a < 0)).view(H, n, d // 2, 2)
+            + 8 * (a < 0).to(torch.uint8)).view(H, n, d // 2, 2)
     return torch.cat(((code[..., 0] | code[..., 1] << 4).reshape(-1), (e + 127).to(torch.uint8).reshape(-1)))
 
 
