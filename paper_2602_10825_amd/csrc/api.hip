@@ -249,7 +249,7 @@ int flowcache_attend(const void* q, const void* k_new, const void* v_new, void* 
     std::memcpy(at.active_off, active_off, sizeof(int32_t) * A);
     at.rec_idx = recompute_idx; at.n_rec = n_recompute; at.scale = scale;
     at.ws = workspace; at.ws_bytes = workspace ? workspace_bytes : 0;
-    st = (dtype == FC_BF16) ? fc_launch_attend_bf16(at, nullptr, s) : fc_launch_attend_f32(at, s);
+    st = (dtype == FC_BF16) ? fc_launch_attend_bf16(at, s) : fc_launch_attend_f32(at, s);
     if (st != FC_OK) return st;
 
     if (mass) {
@@ -395,14 +395,14 @@ int flowcache_attend_kv4(const void* q, const void* k_new, const void* v_new, co
     FcAttendArgs at{};
     at.q = q; at.out = out; at.lse = lse; at.k_cache = k_cache; at.v_cache = v_cache;
     at.head_stride = kv_head_stride; at.tok_stride = kv_tok_stride; at.dtype = dtype;
-    at.H_q = H_q; at.H_k = H_k; at.d = d; at.L_c = L_c; at.L_clean = L_clean; at.A = A;
+    at.H_q = H_q; at.H_k = H_k; at.d = d; at.L_c = L_c; at.A = A;
     std::memcpy(at.active_off, active_off, sizeof(int32_t) * A);
     at.rec_idx = recompute_idx; at.n_rec = n_recompute;
     at.scale = softmax_scale > 0.f ? softmax_scale : 1.0f / std::sqrt((float)d);
     at.ws = workspace; at.ws_bytes = workspace ? workspace_bytes : 0;
     const int64_t rows = L_clean > 0 ? capacity4 : 0;
-    const FcKv4 clean4{(const uint8_t*)k4, (const uint8_t*)v4, rows * (d / 2), rows * (d / 32), H_k * rows * (d / 2)};
-    return fc_launch_attend_bf16(at, &clean4, (hipStream_t)stream);
+    const FcKv4 clean4{(const uint8_t*)k4, (const uint8_t*)v4, rows * (d / 2), rows * (d / 32), H_k * rows * (d / 2), L_clean};
+    return fc_launch_attend_kv4(at, clean4, (hipStream_t)stream);
 }
 
 // ------------------------------------------------------------------ kv_compress

@@ -46,52 +46,13 @@
 // keys 53 / 18; 12 x 128, 600 rows on 5200 keys 126 / 40, 1500 rows on 51689 keys 1141 / 433, 256
 // rows on 49201 keys 1076 / 106; 2 x 64, 278 rows on 60724 keys 982 / 36; 24 x 64, 2 chunks of 2040
 // rows on 18360 keys (1.5 rounds of units) 550 / 451.
-#include <utility>
-
-#include "attend_split.hpp"
-#include "kv4.hpp"
+#include "attend_bf16.hpp"
 
 namespace {
 
-typedef __bf16 bf16x8_t __attribute__((ext_vector_type(8)));
-typedef __bf16 bf16x2_t __attribute__((ext_vector_type(2)));
-typedef float f32x16_t __attribute__((ext_vector_type(16)));
-typedef float f32x4_t __attribute__((ext_vector_type(4)));
-
-constexpr int BQ = kWideRows;   // query rows per workgroup
-constexpr int BK = 64;       // keys per tile
-
-constexpr int NT = 64 * (BQ / 32);   // 8 wavefronts of 32 query rows, two per SIMD
-
-// f(0), ..., f(N - 1) with the argument a compile-time constant: every choice made on it is made when
-// the loop is written out
-template <int N, typename F, int... I>
-__device__ __forceinline__ void static_for_impl(F&& f, std::integer_sequence<int, I...>) {
-    (f(std::integral_constant<int, I>()), ...);
-}
-template <int N, typename F>
-__device__ __forceinline__ void static_for(F&& f) {
-    static_for_impl<N>(f, std::make_integer_sequence<int, N>());
-}
-
 template <int D>
-struct WideSmem {
-    static constexpr int KROW = D + 8;        // padded K row (bf16): 16-byte fragment reads of 16
-                                              // consecutive keys fall in distinct banks
-    static constexpr int VROW = D + 32;       // padded V row: the 4 key rows of one transposing
-                                              // load fall in disjoint bank quarters
-    __attribute__((aligned(16))) bf16_t K[4][BK * KROW];
-    __attribute__((aligned(16))) bf16_t V[2][BK * VROW];
-    int seg_start[FC_MAX_ACTIVE + 2], seg_len[FC_MAX_ACTIVE + 2];
-    int seg_first, off_first, n_tiles;
-};
-
-// With KV4 the clean region's tiles come from the 4-bit buffers `x` (kv4.hpp) and the caches hold the slots alone.  A
-// tile's codes are turned into bf16 on their way into LDS (exactly: the values have two bits), so that everything
-// behind is the same.  The clean region is the first segment and never one with a slot.
-template <int D, bool KV4>
 __device__ __forceinline__ void attend_wide(const FcAttendArgs& a, const FcAttendPlan& p, uint32_t valid,
-                                            WideSmem<D>& sm, float* parts, const FcKv4& x) {
+                                            WideSmem<D>& sm, float* parts) {
     constexpr int KS = D / 16;        // contraction steps of Q K^T
     constexpr int DVB = D / 32;       // 32-wide blocks of the value dimension
     constexpr int KROW = WideSmem<D>::KROW, VROW = WideSmem<D>::VROW;
@@ -132,7 +93,7 @@ __device__ __forceinline__ void attend_wide(const FcAttendArgs& a, const FcAtten
             int start = (sgi < 0) ? 0 : a.active_off[sgi];
             int len = (sgi < 0) ? a.L_clean : a.L_c;
             ++sgi;
-            while ((!KV4 || sgi > 0) && sgi <= c && a.active_off[sgi] == start + len) { len += a.L_c; ++sgi; }
+            while (sgi <= c && a.active_off[sgi] == start + len) { len += a.L_c; ++sgi; }
             if (len > 0) { sm.seg_start[n] = start; sm.seg_len[n] = len; ++n; nt += (len + BK - 1) / BK; }
         }
         const int lo = (int)((int64_t)nt * wi.s / wi.S);
@@ -159,16 +120,10 @@ __device__ __forceinline__ void attend_wide(const FcAttendArgs& a, const FcAtten
     // past the end of a segment re-read its last one.  K runs two tiles ahead of V.
     int64_t pos_k, pos_v, pos_q0 = 0, pos_q1 = 0;      // element offsets of the tiles' first rows
     int nv_k, nv_v, nv_q0 = BK, nv_q1 = BK;
-    bool in4_k = false, in4_v = false, in4_q0 = false, in4_q1 = false;   // a tile of the 4-bit buffers; pos is then a row
     auto step_tile = [&]() {          // K's next tile; V's is the one K had two calls before
         pos_v = pos_q1; nv_v = nv_q1;
         pos_q1 = pos_q0; nv_q1 = nv_q0;
-        if constexpr (KV4) {
-            in4_v = in4_q1;
-            in4_q1 = in4_q0;
-            in4_q0 = in4_k = seg == 0 && a.L_clean > 0;
-        }
-        pos_k = KV4 && in4_k ? (int64_t)t0 : (int64_t)(start + t0) * a.tok_stride;
+        pos_k = (int64_t)(start + t0) * a.tok_stride;
         nv_k = len - t0 < BK ? len - t0 : BK;
         pos_q0 = pos_k; nv_q0 = nv_k;
         if (to_step > 0) {
@@ -196,41 +151,6 @@ __device__ __forceinline__ void attend_wide(const FcAttendArgs& a, const FcAtten
         dst = *reinterpret_cast<const u32x4_native*>(b + off);
     };
     const int st_k = ld_row * KROW + ld_col * 8, st_v = ld_row * VROW + ld_col * 8;
-    // The same for either kind of tile.  Of a 4-bit tile a thread has CPT neighbouring codes of one row: codes in the first
-    // registers, their scale's byte in the last.
-    constexpr int CPT = BK * D / NT;
-    const int row4 = tid / (D / CPT), col4 = tid % (D / CPT) * CPT;
-    const uint8_t *k4 = nullptr, *v4 = nullptr;
-    if constexpr (KV4) { k4 = x.k + (int64_t)hk * x.head_codes; v4 = x.v + (int64_t)hk * x.head_codes; }
-    const int64_t to_scales = KV4 ? x.scales_at + (int64_t)hk * (x.head_scales - x.head_codes) : 0;
-    auto load_tile = [&](u32x4_native (&dst)[LD], const bf16_t* base, const uint8_t* base4, bool in4, int64_t pos, int nv) {
-        if (KV4 && in4) {
-            const int row = row4 < nv ? row4 : nv - 1;
-            const uint8_t* codes = base4 + pos * (D / 2);
-            const uint8_t* scales = base4 + to_scales + pos * (D / 32);
-            const uint32_t at = (uint32_t)(row * (D / 2) + col4 / 2);
-            if constexpr (CPT == 16) {
-                const uint2 w = *reinterpret_cast<const uint2*>(codes + at);
-                dst[0].x = w.x; dst[0].y = w.y;
-            } else {
-                dst[0].x = *reinterpret_cast<const uint32_t*>(codes + at);
-            }
-            dst[0].w = scales[(uint32_t)(row * (D / 32) + col4 / 32)];
-        } else {
-#pragma unroll
-            for (int i = 0; i < LD; ++i) load_rows(dst[i], base, pos, nv, i);
-        }
-    };
-    auto store_tile = [&](bf16_t* tile, const u32x4_native (&src)[LD], bool in4, const int ROW) {
-        if (KV4 && in4) {
-            bf16_t* to = tile + row4 * ROW + col4;
-            *reinterpret_cast<u32x4_native*>(to) = fc_kv4_to_bf16(src[0].x, src[0].w);
-            if constexpr (CPT == 16) *reinterpret_cast<u32x4_native*>(to + 8) = fc_kv4_to_bf16(src[0].y, src[0].w);
-        } else {
-#pragma unroll
-            for (int i = 0; i < LD; ++i) *reinterpret_cast<u32x4_native*>(tile + (ld_row + i * RPP) * ROW + ld_col * 8) = src[i];
-        }
-    };
     // per-lane offsets of the fragment reads.  Transposing V read: lane s of a 16-lane group addresses
     // key (s/4), dv 4*(s%4) of the group's 4-key x 16-dv patch; groups 0/1 cover dv 0-15 / 16-31,
     // lane half = key half
@@ -293,21 +213,7 @@ __device__ __forceinline__ void attend_wide(const FcAttendArgs& a, const FcAtten
     if (nt > 0) {
         // ---- K(0), K(1) into the ring, K(2) and V(0) on their way, S(0); "V(-1)" finite (its P is zero)
         int nv_prev = BK, nv_cur, nv_next;   // valid keys of the tile before S's, of S's and of the next one
-        if constexpr (KV4) {
-            step_tile();
-            nv_cur = nv_k;
-            const bool first4 = in4_k;
-            load_tile(kreg, kbase, k4, in4_k, pos_k, nv_k);
-            step_tile();
-            nv_next = nv_k;
-            load_tile(vreg, kbase, k4, in4_k, pos_k, nv_k);
-            store_tile(sm.K[0], kreg, first4, KROW);
-            store_tile(sm.K[1], vreg, in4_k, KROW);
-            for (int i = tid; i < BK * VROW / 8; i += NT) reinterpret_cast<uint4*>(sm.V[1])[i] = make_uint4(0, 0, 0, 0);
-            step_tile();
-            load_tile(kreg, kbase, k4, in4_k, pos_k, nv_k);
-            load_tile(vreg, vbase, v4, in4_v, pos_v, nv_v);
-        } else {
+        {
             step_tile();
             nv_cur = nv_k;
 #pragma unroll
@@ -393,21 +299,12 @@ __device__ __forceinline__ void attend_wide(const FcAttendArgs& a, const FcAtten
                         pack4(wt[(4 * q) & 7], wt[(4 * q + 1) & 7], wt[(4 * q + 2) & 7], wt[(4 * q + 3) & 7], q);
                 });
                 // staging: K(j+2), V(j) to LDS, then the loads of K(j+3), V(j+1)
-                if constexpr (KV4) {
-                    if constexpr (f == 2) store_tile(sm.K[(j + 2) & 3], kreg, in4_k, KROW);
-                    if constexpr (f == 3) {
-                        store_tile(sm.V[j & 1], vreg, in4_v, VROW);
-                        step_tile();
-                    }
-                    if constexpr (f == 4) load_tile(kreg, kbase, k4, in4_k, pos_k, nv_k);
-                    if constexpr (f == 5) load_tile(vreg, vbase, v4, in4_v, pos_v, nv_v);
-                }
-                if constexpr (!KV4 && f >= 2 && f < 2 + LD)
+                if constexpr (f >= 2 && f < 2 + LD)
                     *reinterpret_cast<u32x4_native*>(Kw + (f - 2) * RPP * KROW) = kreg[f - 2];
-                if constexpr (!KV4 && f >= 2 + LD && f < 2 + 2 * LD)
+                if constexpr (f >= 2 + LD && f < 2 + 2 * LD)
                     *reinterpret_cast<u32x4_native*>(Vw + (f - 2 - LD) * RPP * VROW) = vreg[f - 2 - LD];
-                if constexpr (!KV4 && f == 2 + 2 * LD) step_tile();
-                if constexpr (!KV4 && f >= 2 + 2 * LD && f < 2 + 3 * LD) {
+                if constexpr (f == 2 + 2 * LD) step_tile();
+                if constexpr (f >= 2 + 2 * LD && f < 2 + 3 * LD) {
                     load_rows(kreg[f - 2 - 2 * LD], kbase, pos_k, nv_k, f - 2 - 2 * LD);
                     load_rows(vreg[f - 2 - 2 * LD], vbase, pos_v, nv_v, f - 2 - 2 * LD);
                 }
@@ -523,9 +420,9 @@ struct NarrowSmem {
     Segments sg;
 };
 
-template <int D, bool KV4>
+template <int D>
 __device__ __forceinline__ void attend_narrow(const FcAttendArgs& a, const FcAttendPlan& p, uint32_t valid,
-                                              NarrowSmem<D>& sm, float* parts, const FcKv4& x) {
+                                              NarrowSmem<D>& sm, float* parts) {
     constexpr int KS = D / 16;           // contraction steps of Q K^T
     constexpr int DVB = D / 32;          // 32-wide blocks of the value dimension
     constexpr int KROW = NarrowSmem<D>::KROW, VROW = NarrowSmem<D>::VROW, OROW = NarrowSmem<D>::OROW;
@@ -542,7 +439,7 @@ __device__ __forceinline__ void attend_narrow(const FcAttendArgs& a, const FcAtt
     const int wave = __builtin_amdgcn_readfirstlane(tid >> 6), lane = tid & 63;
     const int l32 = lane & 31, hh = lane >> 5;
     const float c2 = a.scale * 1.4426950408889634f;
-    if (tid == 0) list_segments<KV4>(a, it.c, sg);
+    if (tid == 0) list_segments(a, it.c, sg);
 
     // B operand of S^T = K Q^T: lane holds Q[q = l32][16 step + 8 hh .. + 8)
     bf16x8_t qf[KS];
@@ -570,13 +467,6 @@ __device__ __forceinline__ void attend_narrow(const FcAttendArgs& a, const FcAtt
 
     u32x4_native kr[LD], vr[LD];
     int seg = 0, nvalid = 0;
-    // a tile of the 4-bit buffers: a lane has whole blocks of 32 codes, BPR of which are a row, and their scales' bytes behind
-    constexpr int BPR = D / 32, LD4 = 32 * BPR / FC_WAVE;
-    static_assert(2 * LD4 <= LD, "codes and scales fit the registers of a bf16 tile");
-    bool in4 = false;
-    const uint8_t *k4 = nullptr, *v4 = nullptr;
-    if constexpr (KV4) { k4 = x.k + (int64_t)hk * x.head_codes; v4 = x.v + (int64_t)hk * x.head_codes; }
-    const int64_t to_scales = KV4 ? x.scales_at + (int64_t)hk * (x.head_scales - x.head_codes) : 0;
     const int ld_row = lane / VPR, ld_col = lane % VPR;
     // tile tt -> registers, by rows; a row past the end of its segment re-reads the last one
     auto fetch = [&](int tt) {
@@ -585,22 +475,6 @@ __device__ __forceinline__ void attend_narrow(const FcAttendArgs& a, const FcAtt
         const int left = __builtin_amdgcn_readfirstlane(sg.len[seg]) - off;
         const int64_t pos = (int64_t)(__builtin_amdgcn_readfirstlane(sg.start[seg]) + off) * a.tok_stride;
         nvalid = left < 32 ? left : 32;
-        if constexpr (KV4) {
-            in4 = seg == 0 && a.L_clean > 0;
-            if (in4) {
-#pragma unroll
-                for (int i = 0; i < LD4; ++i) {
-                    int row = i * (FC_WAVE / BPR) + lane / BPR;
-                    row = off + (row < nvalid ? row : nvalid - 1);
-                    const int64_t at = (int64_t)row * BPR + lane % BPR;       // block of 32 codes
-                    kr[i] = *reinterpret_cast<const u32x4_native*>(k4 + at * 16);
-                    vr[i] = *reinterpret_cast<const u32x4_native*>(v4 + at * 16);
-                    kr[LD4 + i].x = k4[to_scales + at];
-                    vr[LD4 + i].x = v4[to_scales + at];
-                }
-                return;
-            }
-        }
         const char* kt = reinterpret_cast<const char*>(kbase + pos);
         const char* vt = reinterpret_cast<const char*>(vbase + pos);
 #pragma unroll
@@ -618,23 +492,11 @@ __device__ __forceinline__ void attend_narrow(const FcAttendArgs& a, const FcAtt
     if (t < t_end) fetch(t);
     while (t < t_end) {
         // the wavefront's own tile: its LDS accesses are served in order, no barrier is needed
-        if (KV4 && in4) {
 #pragma unroll
-            for (int i = 0; i < LD4; ++i) {
-                const int row = i * (FC_WAVE / BPR) + lane / BPR, col = lane % BPR * 32;
-#pragma unroll
-                for (int j = 0; j < 4; ++j) {
-                    *reinterpret_cast<u32x4_native*>(&kw[row * KROW + col + 8 * j]) = fc_kv4_to_bf16(kr[i][j], kr[LD4 + i].x);
-                    *reinterpret_cast<u32x4_native*>(&vw[row * VROW + col + 8 * j]) = fc_kv4_to_bf16(vr[i][j], vr[LD4 + i].x);
-                }
-            }
-        } else {
-#pragma unroll
-            for (int i = 0; i < LD; ++i) {
-                const int row = i * (FC_WAVE / VPR) + ld_row;
-                *reinterpret_cast<u32x4_native*>(&kw[row * KROW + ld_col * 8]) = kr[i];
-                *reinterpret_cast<u32x4_native*>(&vw[row * VROW + ld_col * 8]) = vr[i];
-            }
+        for (int i = 0; i < LD; ++i) {
+            const int row = i * (FC_WAVE / VPR) + ld_row;
+            *reinterpret_cast<u32x4_native*>(&kw[row * KROW + ld_col * 8]) = kr[i];
+            *reinterpret_cast<u32x4_native*>(&vw[row * VROW + ld_col * 8]) = vr[i];
         }
         const int nv = nvalid;
         t += kSplitWaves;
@@ -708,8 +570,8 @@ __device__ __forceinline__ void attend_narrow(const FcAttendArgs& a, const FcAtt
 }
 
 // WIDE and NARROW say which of the two bodies some recompute count of this launch asks for.
-template <int D, bool WIDE, bool NARROW, bool KV4>
-__device__ __forceinline__ void attend_block(const FcAttendArgs& a, const FcAttendPlan& p, float* parts, const FcKv4& x) {
+template <int D, bool WIDE, bool NARROW>
+__global__ __launch_bounds__(NT) void attend_bf16_kernel(FcAttendArgs a, FcAttendPlan p, float* parts) {
     static_assert(NT == kSplitThreads, "both bodies run on the same block");
     const uint32_t valid = valid_blocks(a);
     const int R = __popc(valid);
@@ -720,40 +582,24 @@ __device__ __forceinline__ void attend_block(const FcAttendArgs& a, const FcAtte
     };
     __shared__ __attribute__((aligned(16))) char raw[WIDE && NARROW ? sizeof(Smem) : WIDE ? sizeof(WideSmem<D>) : sizeof(NarrowSmem<D>)];
     if (WIDE && (!NARROW || !p.narrow[R - 1]))
-        attend_wide<D, KV4>(a, p, valid, *reinterpret_cast<WideSmem<D>*>(raw), parts, x);
+        attend_wide<D>(a, p, valid, *reinterpret_cast<WideSmem<D>*>(raw), parts);
     else if (NARROW)
-        attend_narrow<D, KV4>(a, p, valid, *reinterpret_cast<NarrowSmem<D>*>(raw), parts, x);
-}
-template <int D, bool WIDE, bool NARROW>
-__global__ __launch_bounds__(NT) void attend_bf16_kernel(FcAttendArgs a, FcAttendPlan p, float* parts) {
-    attend_block<D, WIDE, NARROW, false>(a, p, parts, FcKv4{});
-}
-template <int D, bool WIDE, bool NARROW>
-__global__ __launch_bounds__(NT) void attend_kv4_kernel(FcAttendArgs a, FcAttendPlan p, float* parts, FcKv4 x) {
-    attend_block<D, WIDE, NARROW, true>(a, p, parts, x);
-}
-
-template <int D, bool WIDE, bool NARROW>
-void launch_form(const FcAttendArgs& a, const FcAttendPlan& p, const FcKv4* x, hipStream_t s) {
-    if (x)
-        attend_kv4_kernel<D, WIDE, NARROW><<<p.grid, NT, 0, s>>>(a, p, (float*)a.ws, *x);
-    else
-        attend_bf16_kernel<D, WIDE, NARROW><<<p.grid, NT, 0, s>>>(a, p, (float*)a.ws);
+        attend_narrow<D>(a, p, valid, *reinterpret_cast<NarrowSmem<D>*>(raw), parts);
 }
 
 template <int D>
-int launch_bf16(const FcAttendArgs& a, const FcKv4* x, hipStream_t s) {
+int launch_bf16(const FcAttendArgs& a, hipStream_t s) {
     FcAttendPlan p = fc_attend_plan_bf16(a.A, a.L_c, a.L_clean, a.H_q, D, true);
     if (!fc_room_for_partials(a.ws, a.ws_bytes, p.parts, D))
         p = fc_attend_plan_bf16(a.A, a.L_c, a.L_clean, a.H_q, D, false);
     bool wide = false, narrow = false;
     for (int R = 0; R < a.A; ++R) (p.narrow[R] ? narrow : wide) = true;
     if (!narrow)
-        launch_form<D, true, false>(a, p, x, s);
+        attend_bf16_kernel<D, true, false><<<p.grid, NT, 0, s>>>(a, p, (float*)a.ws);
     else if (!wide)
-        launch_form<D, false, true>(a, p, x, s);
+        attend_bf16_kernel<D, false, true><<<p.grid, NT, 0, s>>>(a, p, (float*)a.ws);
     else
-        launch_form<D, true, true>(a, p, x, s);
+        attend_bf16_kernel<D, true, true><<<p.grid, NT, 0, s>>>(a, p, (float*)a.ws);
     FC_LAUNCH_CHECK();
     if (p.merge_grid > 0) {
         attend_merge_kernel<bf16_t, D><<<p.merge_grid, 256, 0, s>>>(a, p, (const float*)a.ws);
@@ -764,8 +610,8 @@ int launch_bf16(const FcAttendArgs& a, const FcKv4* x, hipStream_t s) {
 
 }  // namespace
 
-int fc_launch_attend_bf16(const FcAttendArgs& a, const FcKv4* clean4, hipStream_t s) {
-    if (a.d == 128) return launch_bf16<128>(a, clean4, s);
-    if (a.d == 64) return launch_bf16<64>(a, clean4, s);
+int fc_launch_attend_bf16(const FcAttendArgs& a, hipStream_t s) {
+    if (a.d == 128) return launch_bf16<128>(a, s);
+    if (a.d == 64) return launch_bf16<64>(a, s);
     return FC_UNSUPPORTED;
 }

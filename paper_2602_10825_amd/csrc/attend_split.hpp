@@ -277,20 +277,18 @@ __device__ __forceinline__ WideItem wide_item(const FcAttendArgs& a, const FcAtt
 }
 
 // Visible key segments of chunk c (clean region, then active chunks 0..c; adjacent ones merged)
-// with the number of 32-key tiles before each.  Filled by one thread.  A clean region that lies in a buffer of its own
-// (CLEAN_APART) is never merged with a slot.
+// with the number of 32-key tiles before each.  Filled by one thread.
 struct Segments {
     int n;
     int start[FC_MAX_ACTIVE + 1], len[FC_MAX_ACTIVE + 1], tile0[FC_MAX_ACTIVE + 2];
 };
-template <bool CLEAN_APART = false>
 __device__ __forceinline__ void list_segments(const FcAttendArgs& a, int c, Segments& sg) {
     int n = 0, sgi = -1, t = 0;
     while (sgi <= c) {
         const int start = (sgi < 0) ? 0 : a.active_off[sgi];
         int len = (sgi < 0) ? a.L_clean : a.L_c;
         ++sgi;
-        while ((!CLEAN_APART || sgi > 0) && sgi <= c && a.active_off[sgi] == start + len) { len += a.L_c; ++sgi; }
+        while (sgi <= c && a.active_off[sgi] == start + len) { len += a.L_c; ++sgi; }
         if (len > 0) {
             sg.start[n] = start; sg.len[n] = len; sg.tile0[n] = t;
             t += (len + 31) / 32;
