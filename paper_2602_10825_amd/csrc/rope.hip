@@ -13,6 +13,7 @@ namespace {
 
 constexpr int kThreads = 256;
 constexpr int kWaves = kThreads / FC_WAVE;
+constexpr int kAhead = 4;
 
 // Sum over groups of G neighbouring lanes, in all of them.
 template <int G>
@@ -26,74 +27,65 @@ __device__ __forceinline__ float group_sum(float v) {
     return v;
 }
 
-// A lane's V elements: pairs are neighbours (HALVES: one half from each side of the head).
+// A lane's 16 bytes of a head, as two halves of the pairs' elements: neighbours (HALVES: one from each side of the head).
 template <typename T, int D, bool HALVES>
 struct Part {
-    static constexpr int V = Elem<T>::kVec, G = D / V;
-    float a[V / 2], b[V / 2];
-    __device__ __forceinline__ void load(const T* row, int l) {
+    static constexpr int V = Elem<T>::kVec, G = D / V, NP = V / 2;
+    static __device__ __forceinline__ uint4 load(const T* head, int l) {
         if constexpr (HALVES) {
-            load_half(row + l * (V / 2), a);
-            load_half(row + D / 2 + l * (V / 2), b);
+            const uint2 a = *reinterpret_cast<const uint2*>(head + l * NP), b = *reinterpret_cast<const uint2*>(head + D / 2 + l * NP);
+            return make_uint4(a.x, a.y, b.x, b.y);
         } else {
-            float f[V];
-            unpack16(*reinterpret_cast<const uint4*>(row + l * V), f, T());
-#pragma unroll
-            for (int i = 0; i < V / 2; ++i) { a[i] = f[2 * i]; b[i] = f[2 * i + 1]; }
+            return *reinterpret_cast<const uint4*>(head + l * V);
         }
     }
-    __device__ __forceinline__ void store(T* row, int l) const {
+    static __device__ __forceinline__ void store(T* head, int l, const uint4& u) {
         if constexpr (HALVES) {
-            store_half(row + l * (V / 2), a);
-            store_half(row + D / 2 + l * (V / 2), b);
-        } else if constexpr (V == 8) {
-            uint4 u;
-            u.x = pack2(a[0], b[0]); u.y = pack2(a[1], b[1]); u.z = pack2(a[2], b[2]); u.w = pack2(a[3], b[3]);
-            *reinterpret_cast<uint4*>(row + l * V) = u;
+            *reinterpret_cast<uint2*>(head + l * NP) = make_uint2(u.x, u.y);
+            *reinterpret_cast<uint2*>(head + D / 2 + l * NP) = make_uint2(u.z, u.w);
         } else {
-            *reinterpret_cast<float4*>(row + l * V) = make_float4(a[0], b[0], a[1], b[1]);
+            *reinterpret_cast<uint4*>(head + l * V) = u;
         }
     }
-    static __device__ __forceinline__ uint32_t pack2(float x, float y) {
-        return (uint32_t)f32_to_bf16(x) | ((uint32_t)f32_to_bf16(y) << 16);
-    }
-    static __device__ __forceinline__ void load_half(const bf16_t* p, float* f) {
-        const uint2 u = *reinterpret_cast<const uint2*>(p);
-        f[0] = bf16lo_to_f32(u.x); f[1] = bf16hi_to_f32(u.x); f[2] = bf16lo_to_f32(u.y); f[3] = bf16hi_to_f32(u.y);
-    }
-    static __device__ __forceinline__ void load_half(const float* p, float* f) {
-        const float2 u = *reinterpret_cast<const float2*>(p);
-        f[0] = u.x; f[1] = u.y;
-    }
-    static __device__ __forceinline__ void store_half(bf16_t* p, const float* f) {
-        *reinterpret_cast<uint2*>(p) = make_uint2(pack2(f[0], f[1]), pack2(f[2], f[3]));
-    }
-    static __device__ __forceinline__ void store_half(float* p, const float* f) { *reinterpret_cast<float2*>(p) = make_float2(f[0], f[1]); }
+    // pair i of the lane: elements first(i) and second(i) of the 16 bytes
+    static constexpr __device__ int first(int i) { return HALVES ? i : 2 * i; }
+    static constexpr __device__ int second(int i) { return HALVES ? NP + i : 2 * i + 1; }
+    // ... and of the head
+    static __device__ __forceinline__ int first_at(int l, int i) { return HALVES ? l * NP + i : 2 * (l * NP + i); }
+    static __device__ __forceinline__ int second_at(int l, int i) { return HALVES ? D / 2 + l * NP + i : 2 * (l * NP + i) + 1; }
 };
+__device__ __forceinline__ uint4 pack16(const float (&f)[8], bf16_t) {
+    auto two = [](float x, float y) { return (uint32_t)f32_to_bf16(x) | ((uint32_t)f32_to_bf16(y) << 16); };
+    return make_uint4(two(f[0], f[1]), two(f[2], f[3]), two(f[4], f[5]), two(f[6], f[7]));
+}
+__device__ __forceinline__ uint4 pack16(const float (&f)[4], float) {
+    return make_uint4(__float_as_uint(f[0]), __float_as_uint(f[1]), __float_as_uint(f[2]), __float_as_uint(f[3]));
+}
 
-// One wavefront takes the heads of one token, 64 / G of them at a time (`passes` first .. last): queries, then keys, then
-// values.  Its lanes have the same place in every head, so a token's sines and cosines are computed once for all of them.
+// A group of G lanes takes one token and goes through its heads, one per pass: queries, then keys, then values (a launch of few
+// tokens deals a token's passes to several groups).  A lane has the same place in every head, so it computes its sines and cosines
+// once; the wavefront's 64 / G tokens are neighbours, and so are the rows of a cache that it writes.  kAhead passes are read
+// before the first of them is worked on.
 template <typename T, int D, bool HALVES>
 __global__ __launch_bounds__(kThreads) void qk_norm_rope_kernel(FcRopeArgs a, int slices) {
     typedef Part<T, D, HALVES> P;
-    constexpr int G = P::G, PER = FC_WAVE / G, NP = P::V / 2;
+    constexpr int G = P::G, PER = FC_WAVE / G, NP = P::NP;
     const int r = blockIdx.y;
     if (r >= *a.n_rec || r >= a.A) return;
     const int c = a.rec_idx[r];
     if ((unsigned)c >= (unsigned)a.A) return;
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63;
-    const int64_t item = (int64_t)blockIdx.x * kWaves + wave;
-    const int n = (int)(item / slices), slice = (int)(item % slices);
+    const int item = blockIdx.x * kWaves + wave;
+    const int n = item / slices * PER + lane / G, slice = item % slices, l = lane % G;
     if (n >= a.L_c) return;
-    const int l = lane % G, sub = lane / G;
-    const int nq = (a.H_q + PER - 1) / PER, nk = (a.H_k + PER - 1) / PER, nv = a.v ? nk : 0;
-    const int total = nq + nk + nv;
+    const int total = a.H_q + (a.v ? 2 : 1) * a.H_k;
     const int first = (int)((int64_t)total * slice / slices), last = (int)((int64_t)total * (slice + 1) / slices);
     const int64_t row = (int64_t)r * a.L_c + n;
     const int64_t slot = (int64_t)(a.active_off[c] + n) * a.tok_stride;
+    const T *q = (const T*)a.q + row * a.q_stride, *k = (const T*)a.k + row * a.kv_stride, *v = (const T*)a.v + row * a.kv_stride;
 
-    float cs[NP], sn[NP], w[P::V];
-    if (first < nq + nk) {
+    float cs[NP], sn[NP], wq[P::V], wk[P::V];
+    if (first < a.H_q + a.H_k) {
         const int frame = n / (a.grid_h * a.grid_w), in = n - frame * (a.grid_h * a.grid_w);
         const double pt = (double)a.frame0[c] + frame, ph = in / a.grid_w, pw = in % a.grid_w;
 #pragma unroll
@@ -102,56 +94,65 @@ __global__ __launch_bounds__(kThreads) void qk_norm_rope_kernel(FcRopeArgs a, in
             // in revolutions: whole ones are dropped in 64 bits, so far positions lose nothing
             const double t = (p < a.pairs_t ? pt : p < a.pairs_th ? ph : pw) * a.turns[p];
             sincospif(2.0f * (float)(t - rint(t)), &sn[i], &cs[i]);
+            wq[P::first(i)] = a.q_weight ? a.q_weight[P::first_at(l, i)] : 1.0f;
+            wq[P::second(i)] = a.q_weight ? a.q_weight[P::second_at(l, i)] : 1.0f;
+            wk[P::first(i)] = a.k_weight ? a.k_weight[P::first_at(l, i)] : 1.0f;
+            wk[P::second(i)] = a.k_weight ? a.k_weight[P::second_at(l, i)] : 1.0f;
         }
     }
-    for (int pass = first; pass < last; ++pass) {
-        const bool is_q = pass < nq, is_k = !is_q && pass < nq + nk;
-        const int h = (pass - (is_q ? 0 : is_k ? nq : nq + nk)) * PER + sub;
-        if (h >= (is_q ? a.H_q : a.H_k)) continue;
-        const T* src = is_q ? (const T*)a.q + row * a.q_stride : (is_k ? (const T*)a.k : (const T*)a.v) + row * a.kv_stride;
-        T* dst = is_q ? (T*)a.q_out + (row * a.H_q + h) * D : (is_k ? (T*)a.k_cache : (T*)a.v_cache) + h * a.head_stride + slot;
-        src += h * D;
-        if (!is_q && !is_k) {
-            *reinterpret_cast<uint4*>(dst + l * P::V) = *reinterpret_cast<const uint4*>(src + l * P::V);
-            continue;
+    for (int pass0 = first; pass0 < last; pass0 += kAhead) {
+        uint4 u[kAhead];
+#pragma unroll
+        for (int e = 0; e < kAhead; ++e) {
+            const int pass = pass0 + e < last ? pass0 + e : last - 1;        // (past the end: read again, not written)
+            const bool is_q = pass < a.H_q, is_k = pass < a.H_q + a.H_k;
+            const int h = pass - (is_q ? 0 : is_k ? a.H_q : a.H_q + a.H_k);
+            u[e] = P::load((is_q ? q : is_k ? k : v) + h * D, l);
         }
-        P x;
-        x.load(src, l);
-        if (a.norm) {
-            const float* wp = is_q ? a.q_weight : a.k_weight;
-            float ss = 0.f;
 #pragma unroll
-            for (int i = 0; i < NP; ++i) ss = fmaf(x.a[i], x.a[i], fmaf(x.b[i], x.b[i], ss));
-            const float inv = rsqrtf(group_sum<G>(ss) * (1.0f / D) + a.eps);
+        for (int e = 0; e < kAhead; ++e) {
+            const int pass = pass0 + e;
+            if (pass >= last) break;
+            const bool is_q = pass < a.H_q, is_k = pass < a.H_q + a.H_k;
+            const int h = pass - (is_q ? 0 : is_k ? a.H_q : a.H_q + a.H_k);
+            if (is_k) {                                                      // a query or a key
+                float f[P::V];
+                unpack16(u[e], f, T());
+                if (a.norm) {
+                    float ss = 0.f;
 #pragma unroll
-            for (int i = 0; i < NP; ++i) {
-                x.a[i] *= inv; x.b[i] *= inv;
-                if (wp) {
-                    x.a[i] *= wp[HALVES ? l * NP + i : 2 * (l * NP + i)];
-                    x.b[i] *= wp[HALVES ? D / 2 + l * NP + i : 2 * (l * NP + i) + 1];
+                    for (int i = 0; i < P::V; ++i) ss = fmaf(f[i], f[i], ss);
+                    const float inv = rsqrtf(group_sum<G>(ss) * (1.0f / D) + a.eps);
+#pragma unroll
+                    for (int i = 0; i < P::V; ++i) f[i] = f[i] * inv * (is_q ? wq[i] : wk[i]);
                 }
-            }
-        }
 #pragma unroll
-        for (int i = 0; i < NP; ++i) {
-            const float u = x.a[i] * cs[i] - x.b[i] * sn[i], v = x.a[i] * sn[i] + x.b[i] * cs[i];
-            x.a[i] = u; x.b[i] = v;
+                for (int i = 0; i < NP; ++i) {
+                    const float x = f[P::first(i)], y = f[P::second(i)];
+                    f[P::first(i)] = x * cs[i] - y * sn[i];
+                    f[P::second(i)] = x * sn[i] + y * cs[i];
+                }
+                u[e] = pack16(f, T());
+            }
+            P::store(is_q ? (T*)a.q_out + (row * a.H_q + h) * D : (is_k ? (T*)a.k_cache : (T*)a.v_cache) + h * a.head_stride + slot, l, u[e]);
         }
-        x.store(dst, l);
     }
 }
 
 template <typename T, int D>
 int launch(const FcRopeArgs& a, hipStream_t s) {
-    const int per = FC_WAVE / (D / Elem<T>::kVec);
-    const int passes = (a.H_q + per - 1) / per + (a.v ? 2 : 1) * ((a.H_k + per - 1) / per);
-    int slices = 1;
-    const int64_t blocks = ((int64_t)a.L_c * slices + kWaves - 1) / kWaves;
-    (void)passes;
+    constexpr int per = FC_WAVE / (D / Elem<T>::kVec);        // tokens per wavefront
+    const int total = a.H_q + (a.v ? 2 : 1) * a.H_k;
+    const int64_t groups = (a.L_c + per - 1) / per;
+    // eight wavefronts for every compute unit, if a chunk's passes are so many
+    int64_t slices = (2048 + groups - 1) / groups;
+    slices = slices < total ? slices : total;
+    const int64_t blocks = (groups * slices + kWaves - 1) / kWaves;
+    if (blocks > INT32_MAX / kWaves) return FC_UNSUPPORTED;
     if (a.pairing)
-        qk_norm_rope_kernel<T, D, true><<<dim3((unsigned)blocks, a.A), kThreads, 0, s>>>(a, slices);
+        qk_norm_rope_kernel<T, D, true><<<dim3((unsigned)blocks, a.A), kThreads, 0, s>>>(a, (int)slices);
     else
-        qk_norm_rope_kernel<T, D, false><<<dim3((unsigned)blocks, a.A), kThreads, 0, s>>>(a, slices);
+        qk_norm_rope_kernel<T, D, false><<<dim3((unsigned)blocks, a.A), kThreads, 0, s>>>(a, (int)slices);
     FC_LAUNCH_CHECK();
     return FC_OK;
 }
