@@ -453,29 +453,26 @@ def _empty(shape, dtype, device, stream=None) -> torch.Tensor:
     return torch.empty(shape, dtype=dtype, device=device)
 
 
-def _same_device(call: str, stream, first: torch.Tensor, *others: Optional[torch.Tensor]) -> None:
+def _same_device(call: str, stream, *tensors: Optional[torch.Tensor]) -> None:
     """A kernel runs on the stream's device, by default the current one: tensors of another are refused."""
-    dev = first.device
-    for t in others:
-        if t is not None and t.device != dev:
-            raise ValueError(f"{call}: tensors on {dev} and {t.device}")
-    if dev.type != "cuda":
-        raise ValueError(f"{call}: tensors on {dev}, not on a GPU")
     on = torch._C._cuda_getDevice() if stream is None else stream.device_index
-    if dev.index != on:
-        raise ValueError(f"{call}: tensors on {dev}, the stream on device {on}")
+    for t in tensors:
+        if t is not None and t.get_device() != on:
+            raise ValueError(f"{call}: a tensor on {t.device}, the stream on cuda:{on}")
 
 
 _PAIRINGS = {"interleaved": 0, "halves": 1}
+_Three = ctypes.c_int32 * 3
 
 
-def _heads_of_rows(call: str, name: str, x: torch.Tensor, rows: int, d: int, dtype) -> int:
-    """Elements from row to row of ``[rows, H, d]``, whose heads and elements follow each other."""
-    if x.dim() != 3 or x.shape[0] != rows or x.shape[2] != d or x.dtype != dtype:
-        raise ValueError(f"{call}: {name} is [{rows}, heads, {d}] of {dtype}, got {tuple(x.shape)} of {x.dtype}")
-    if x.stride(2) != 1 or (x.shape[1] > 1 and x.stride(1) != d):
+def _heads_of_rows(call: str, name: str, x: torch.Tensor, rows: int, heads: int, d: int, dtype) -> int:
+    """Elements from row to row of ``[rows, heads, d]``, whose heads and elements follow each other."""
+    if tuple(x.shape) != (rows, heads, d) or x.dtype != dtype:
+        raise ValueError(f"{call}: {name} is [{rows}, {heads}, {d}] of {dtype}, got {tuple(x.shape)} of {x.dtype}")
+    row, head, one = x.stride()
+    if one != 1 or (heads > 1 and head != d):
         raise ValueError(f"{call}: the heads of a row of {name} have to follow each other, got strides {x.stride()}")
-    return x.stride(0) if rows > 1 else max(x.stride(0), x.shape[1] * d)
+    return row if rows > 1 else max(row, heads * d)
 
 
 def flowcache_qk_norm_rope(q: torch.Tensor, k: torch.Tensor, v: Optional[torch.Tensor], k_cache: torch.Tensor,
@@ -494,33 +491,34 @@ def flowcache_qk_norm_rope(q: torch.Tensor, k: torch.Tensor, v: Optional[torch.T
     frame in tokens; ``frame0``: the first frame of each active chunk; weights: float32 ``[d]``."""
     call = "flowcache_qk_norm_rope"
     H_k, capacity, d = k_cache.shape
-    A, H_q, rows = len(active_off), q.shape[1], q.shape[0]
+    A, H_q, rows, dtype = len(active_off), q.shape[1], q.shape[0], k_cache.dtype
     if rows != A * L_c or len(dims) != 3 or len(grid) != 2 or len(frame0) != A:
         raise ValueError(f"{call}: q has A * L_c rows, dims three numbers, grid two, frame0 one per active chunk")
     if pairing not in _PAIRINGS:
         raise ValueError(f"{call}: pairing is one of {sorted(_PAIRINGS)}, got {pairing!r}")
     _same_device(call, stream, q, k, v, k_cache, v_cache, recompute_idx, n_recompute, q_weight, k_weight, q_out)
-    qs = _heads_of_rows(call, "q", q, rows, d, k_cache.dtype)
-    ks = _heads_of_rows(call, "k", k, rows, d, k_cache.dtype)
-    assert k.shape[1] == H_k and k_cache.stride(2) == 1 and (v is None) == (v_cache is None)
+    qs = _heads_of_rows(call, "q", q, rows, H_q, d, dtype)
+    ks = _heads_of_rows(call, "k", k, rows, H_k, d, dtype)
+    strides = k_cache.stride()
+    assert strides[2] == 1 and (v is None) == (v_cache is None)
     if v is not None:
-        if _heads_of_rows(call, "v", v, rows, d, k_cache.dtype) != ks or v.shape[1] != H_k:
-            raise ValueError(f"{call}: k and v have the same heads and row stride")
-        assert v_cache.stride() == k_cache.stride() and v_cache.shape == k_cache.shape and v_cache.dtype == k_cache.dtype
+        if _heads_of_rows(call, "v", v, rows, H_k, d, dtype) != ks:
+            raise ValueError(f"{call}: k and v have the same row stride")
+        assert v_cache.stride() == strides and v_cache.shape == k_cache.shape and v_cache.dtype == dtype
     for w in (q_weight, k_weight):
         if w is not None and (w.dtype != torch.float32 or tuple(w.shape) != (d,) or not w.is_contiguous()):
             raise ValueError(f"{call}: weights are float32 [{d}]")
     if q_out is None:
-        q_out = _empty((rows, H_q, d), q.dtype, q.device, stream)
-    assert q_out.shape == (rows, H_q, d) and q_out.is_contiguous() and q_out.dtype == q.dtype
-    i32 = ctypes.c_int32
+        q_out = _empty((rows, H_q, d), dtype, q.device, stream)
+    else:
+        assert q_out.shape == q.shape and q_out.is_contiguous() and q_out.dtype == dtype
+    per_chunk = ctypes.c_int32 * A
     st = (_lib or lib()).flowcache_qk_norm_rope(
         _ptr(q), qs, _ptr(k), _ptr(v), ks, _dtype_code(k_cache), H_q, H_k, d, int(norm_eps is not None),
-        0.0 if norm_eps is None else float(norm_eps), _ptr(q_weight), _ptr(k_weight),
-        (i32 * 3)(*[int(x) for x in dims]), _PAIRINGS[pairing], float(theta), int(grid[0]), int(grid[1]),
-        (i32 * A)(*[int(x) for x in frame0]), int(L_c), int(L_clean), A, (i32 * A)(*[int(x) for x in active_off]),
-        _ptr(recompute_idx), _ptr(n_recompute), _ptr(q_out), _ptr(k_cache), _ptr(v_cache), k_cache.stride(0),
-        k_cache.stride(1), capacity, _stream(stream))
+        0.0 if norm_eps is None else float(norm_eps), _ptr(q_weight), _ptr(k_weight), _Three(*map(int, dims)),
+        _PAIRINGS[pairing], float(theta), int(grid[0]), int(grid[1]), per_chunk(*map(int, frame0)), int(L_c),
+        int(L_clean), A, per_chunk(*map(int, active_off)), _ptr(recompute_idx), _ptr(n_recompute), _ptr(q_out),
+        _ptr(k_cache), _ptr(v_cache), strides[0], strides[1], capacity, _stream(stream))
     _check(call, st)
     return q_out
 
@@ -533,16 +531,15 @@ def kv4_buffer(H_k: int, capacity4: int, d: int, device="cuda") -> torch.Tensor:
     return torch.empty(nbytes, dtype=torch.uint8, device=device)
 
 
-def _kv4_shapes(call: str, stream, k4, v4, capacity4: int, k_cache, v_cache, *others) -> None:
-    H_k, _, d = k_cache.shape
-    _same_device(call, stream, k_cache, v_cache, k4, v4, *others)
-    assert k_cache.stride(2) == 1 and (v4 is None) == (v_cache is None)
-    assert v_cache is None or (v_cache.stride() == k_cache.stride() and v_cache.shape == k_cache.shape
-                               and v_cache.dtype == k_cache.dtype)
-    need = H_k * int(capacity4) * (d // 2 + d // 32)
+def _kv4_shapes(call: str, k4, v4, capacity4: int, k_cache, v_cache) -> tuple:
+    shape, strides = k_cache.shape, k_cache.stride()
+    assert strides[2] == 1 and (v4 is None) == (v_cache is None)
+    assert v_cache is None or (v_cache.stride() == strides and v_cache.shape == shape and v_cache.dtype == k_cache.dtype)
+    need = shape[0] * int(capacity4) * (shape[2] // 2 + shape[2] // 32)
     for x in (k4, v4):
         if x is not None and (x.dtype != torch.uint8 or not x.is_contiguous() or x.numel() < need):
             raise ValueError(f"{call}: a 4-bit buffer of {capacity4} rows per head is {need} contiguous bytes of uint8")
+    return strides
 
 
 def flowcache_kv4_pack(k_cache: torch.Tensor, v_cache: Optional[torch.Tensor], k4: torch.Tensor,
@@ -552,9 +549,10 @@ def flowcache_kv4_pack(k_cache: torch.Tensor, v_cache: Optional[torch.Tensor], k
     head) in 4 bits, to rows ``pos4 ..`` of the buffers."""
     call = "flowcache_kv4_pack"
     H_k, capacity, d = k_cache.shape
-    _kv4_shapes(call, stream, k4, v4, capacity4, k_cache, v_cache, kept_idx)
+    _same_device(call, stream, k_cache, v_cache, k4, v4, kept_idx)
+    strides = _kv4_shapes(call, k4, v4, capacity4, k_cache, v_cache)
     assert kept_idx is None or (kept_idx.dtype == torch.int32 and kept_idx.is_contiguous() and kept_idx.shape == (H_k, count))
-    st = (_lib or lib()).flowcache_kv4_pack(_ptr(k_cache), _ptr(v_cache), k_cache.stride(0), k_cache.stride(1), capacity,
+    st = (_lib or lib()).flowcache_kv4_pack(_ptr(k_cache), _ptr(v_cache), strides[0], strides[1], capacity,
                                             _dtype_code(k_cache), H_k, d, int(cache_pos), _ptr(kept_idx), int(count),
                                             _ptr(k4), _ptr(v4), int(capacity4), int(pos4), _stream(stream))
     _check(call, st)
@@ -566,10 +564,11 @@ def flowcache_kv4_unpack(k4: torch.Tensor, v4: Optional[torch.Tensor], capacity4
     """What rows ``pos4 .. + count`` of the buffers stand for, to rows ``cache_pos ..`` of the caches."""
     call = "flowcache_kv4_unpack"
     H_k, capacity, d = k_cache.shape
-    _kv4_shapes(call, stream, k4, v4, capacity4, k_cache, v_cache)
+    _same_device(call, stream, k_cache, v_cache, k4, v4)
+    strides = _kv4_shapes(call, k4, v4, capacity4, k_cache, v_cache)
     st = (_lib or lib()).flowcache_kv4_unpack(_ptr(k4), _ptr(v4), int(capacity4), int(pos4), int(count), _ptr(k_cache),
-                                              _ptr(v_cache), k_cache.stride(0), k_cache.stride(1), capacity,
-                                              _dtype_code(k_cache), H_k, d, int(cache_pos), _stream(stream))
+                                              _ptr(v_cache), strides[0], strides[1], capacity, _dtype_code(k_cache),
+                                              H_k, d, int(cache_pos), _stream(stream))
     _check(call, st)
 
 
@@ -585,28 +584,29 @@ def flowcache_attend_kv4(q: torch.Tensor, k_new: Optional[torch.Tensor], v_new: 
     rows, H_q, d = q.shape
     H_k, capacity, _ = k_cache.shape
     A = len(active_off)
+    _same_device(call, stream, q, k_cache, v_cache, k_new, v_new, k4, v4, recompute_idx, n_recompute, out, workspace)
     assert q.is_contiguous() and rows == A * L_c and k_cache.shape[2] == d and (k4 is None) == (v4 is None)
     assert q.dtype == k_cache.dtype and v_cache is not None
     for x in (k_new, v_new):
         assert x is None or (x.is_contiguous() and x.shape == (rows, H_k, d) and x.dtype == q.dtype)
     if k4 is None:
-        _same_device(call, stream, q, k_cache, v_cache)
+        strides = k_cache.stride()
+        assert strides[2] == 1 and v_cache.stride() == strides and v_cache.shape == k_cache.shape
     else:
-        _kv4_shapes(call, stream, k4, v4, capacity4, k_cache, v_cache)
-    _same_device(call, stream, q, k_cache, k_new, v_new, recompute_idx, n_recompute, out, workspace)
+        strides = _kv4_shapes(call, k4, v4, capacity4, k_cache, v_cache)
     if out is None:
         out = _empty(q.shape, q.dtype, q.device, stream)
-    assert out.is_contiguous() and out.shape == q.shape and out.dtype == q.dtype
+    else:
+        assert out.is_contiguous() and out.shape == q.shape and out.dtype == q.dtype
     lse = _empty((H_q, rows), torch.float32, q.device, stream) if want_lse else None
-    off = (ctypes.c_int32 * A)(*[int(x) for x in active_off])
     L = _lib or lib()
     if workspace is None:
         workspace = _workspace(L.flowcache_attend_kv4_workspace(A, L_c, H_q, d), q.device, stream)
     st = L.flowcache_attend_kv4(_ptr(q), _ptr(k_new), _ptr(v_new), _ptr(k4), _ptr(v4), int(capacity4), _ptr(k_cache),
-                                _ptr(v_cache), k_cache.stride(0), k_cache.stride(1), capacity, _dtype_code(q), H_q, H_k,
-                                d, int(L_c), int(L_clean), A, off, _ptr(recompute_idx), _ptr(n_recompute),
-                                float(softmax_scale), _ptr(out), _ptr(lse), _ptr(workspace), workspace.numel(),
-                                _stream(stream))
+                                _ptr(v_cache), strides[0], strides[1], capacity, _dtype_code(q), H_q, H_k, d, int(L_c),
+                                int(L_clean), A, (ctypes.c_int32 * A)(*map(int, active_off)), _ptr(recompute_idx),
+                                _ptr(n_recompute), float(softmax_scale), _ptr(out), _ptr(lse), _ptr(workspace),
+                                workspace.numel(), _stream(stream))
     _check(call, st)
     return {"out": out, "lse": lse}
 

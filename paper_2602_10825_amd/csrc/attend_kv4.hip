@@ -1,5 +1,5 @@
 // Chunk-causal attention on a clean region in 4 bits (kv4.hpp) and the active chunks' bf16 slots: softmax(q K^T scale) V as
-// in attend_bf16.hip, with the same launch plan, merge of partials, bodies and numerics.  The values that codes stand for have
+// in attend_bf16.hip, with the same division of the work, bodies and numerics.  The values that codes stand for have
 // two significant bits: as bf16 operands they are exact, so nothing is rounded that the bf16 kernel does not round.
 //
 // In these kernels FcAttendArgs describes the slots alone (its L_clean is 0); the clean region, x.L_clean rows of the 4-bit
@@ -698,6 +698,59 @@ __device__ __forceinline__ void attend_narrow4(const FcAttendArgs& a, const FcAt
     finish_unit<bf16_t, D, OROW>(a, p, it, sm.o, m_s, l_s, parts);
 }
 
+// The S <= MOST partials of every 32-row unit -> out and lse, as attend_merge_kernel does it but for few rows: a thread has four
+// columns of one row, the factors of a row are computed once, and all of a row's partials are asked for at once, before those
+// (12 x 128, one row on 61201 keys in 20 ranges 15.2 -> MERGE1 us; 256 rows in 8 ranges 17.9 -> MERGE2).
+constexpr int kMergeThreads = 256;
+template <int D>
+struct MergeShape {
+    static constexpr int TPR = D / 4, RPB = kMergeThreads / TPR, BPU = kUnitRows / RPB;   // threads per row, rows per block, blocks per unit
+};
+template <int D, int MOST>
+__global__ __launch_bounds__(kMergeThreads) void merge4_kernel(FcAttendArgs a, FcAttendPlan p, const float* parts) {
+    constexpr int TPR = MergeShape<D>::TPR, RPB = MergeShape<D>::RPB, BPU = MergeShape<D>::BPU;
+    __shared__ float m_s[MOST][RPB], l_s[MOST][RPB];
+    const uint32_t valid = valid_blocks(a);
+    const int R = __popc(valid);
+    if (R == 0) return;
+    const int S = p.splits[R - 1];
+    if (S == 1) return;
+    const int unit = blockIdx.x / BPU, row0 = blockIdx.x % BPU * RPB;
+    int tile, r, h;
+    if (!merge_unit(a, p, valid, R, S, unit, tile, r, h)) return;
+    const int first_row = tile * kUnitRows + row0;
+    if (first_row >= a.L_c) return;
+    const int row = threadIdx.x / TPR, c0 = threadIdx.x % TPR * 4;
+    const float4* src = reinterpret_cast<const float4*>(parts + ((int64_t)unit * S * kUnitRows + row0 + row) * D + c0);
+    float4 v[MOST];
+#pragma unroll
+    for (int s = 0; s < MOST; ++s) v[s] = src[(int64_t)(s < S ? s : S - 1) * (kUnitRows * D / 4)];
+    const float* ml = parts + (int64_t)p.parts * kUnitRows * D + (int64_t)unit * S * 2 * kUnitRows + row0;
+    for (int i = threadIdx.x; i < S * RPB; i += kMergeThreads) {
+        m_s[i / RPB][i % RPB] = ml[i / RPB * 2 * kUnitRows + i % RPB];
+        l_s[i / RPB][i % RPB] = ml[(i / RPB * 2 + 1) * kUnitRows + i % RPB];
+    }
+    __syncthreads();
+    float mt = kNegBig;
+#pragma unroll
+    for (int s = 0; s < MOST; ++s) mt = fmaxf(mt, s < S ? m_s[s][row] : kNegBig);
+    float acc[4] = {0.f, 0.f, 0.f, 0.f}, l = 0.f;
+#pragma unroll
+    for (int s = 0; s < MOST; ++s) {
+        const float f = s < S ? __builtin_amdgcn_exp2f(m_s[s][row] - mt) : 0.f;
+        l = fmaf(s < S ? l_s[s][row] : 0.f, f, l);
+        acc[0] = fmaf(v[s].x, f, acc[0]);
+        acc[1] = fmaf(v[s].y, f, acc[1]);
+        acc[2] = fmaf(v[s].z, f, acc[2]);
+        acc[3] = fmaf(v[s].w, f, acc[3]);
+    }
+    if (first_row + row >= a.L_c) return;
+    const float inv = 1.0f / l;
+    const int64_t grow = (int64_t)r * a.L_c + first_row + row;
+    store_out((bf16_t*)a.out + (grow * a.H_q + h) * D + c0, acc[0] * inv, acc[1] * inv, acc[2] * inv, acc[3] * inv);
+    if (a.lse && c0 == 0) a.lse[(int64_t)h * a.A * a.L_c + grow] = (mt + __builtin_amdgcn_logf(l)) * 0.6931471805599453f;
+}
+
 // WIDE and NARROW say which of the two bodies some recompute count of this launch asks for.
 template <int D, bool WIDE, bool NARROW>
 __global__ __launch_bounds__(NT) void attend_kv4_kernel(FcAttendArgs a, FcAttendPlan p, float* parts, FcKv4 x) {
@@ -732,7 +785,12 @@ int launch_kv4(FcAttendArgs a, const FcKv4& x, hipStream_t s) {
         attend_kv4_kernel<D, true, true><<<p.grid, NT, 0, s>>>(a, p, (float*)a.ws, x);
     FC_LAUNCH_CHECK();
     if (p.merge_grid > 0) {
-        attend_merge_kernel<bf16_t, D><<<p.merge_grid, 256, 0, s>>>(a, p, (const float*)a.ws);
+        const dim3 grid(p.merge_grid * MergeShape<D>::BPU);
+        int most = 1;
+        for (int R = 0; R < a.A; ++R) most = p.splits[R] > most ? p.splits[R] : most;
+        if (most <= 4) merge4_kernel<D, 4><<<grid, kMergeThreads, 0, s>>>(a, p, (const float*)a.ws);
+        else if (most <= 12) merge4_kernel<D, 12><<<grid, kMergeThreads, 0, s>>>(a, p, (const float*)a.ws);
+        else merge4_kernel<D, kMaxSplits><<<grid, kMergeThreads, 0, s>>>(a, p, (const float*)a.ws);
         FC_LAUNCH_CHECK();
     }
     return FC_OK;

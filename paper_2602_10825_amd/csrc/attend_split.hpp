@@ -363,6 +363,36 @@ __device__ __forceinline__ void finish_unit(const FcAttendArgs& a, const FcAtten
         a.lse[(int64_t)it.h * a.A * a.L_c + grow] = (mt + __builtin_amdgcn_logf(l)) * 0.6931471805599453f;
 }
 
+// The 32 rows that unit `unit` of the merge launch stands for: row tile `tile` of head h of row block r.
+__device__ __forceinline__ bool merge_unit(const FcAttendArgs& a, const FcAttendPlan& p, uint32_t valid, int R, int S, int unit,
+                                           int& tile, int& r, int& h) {
+    if (p.narrow[R - 1]) {
+        if (unit >= R * a.H_q * p.tiles) return false;
+        tile = unit % p.tiles;
+        r = block_of_rank(valid, (unit / p.tiles) % R);
+        h = unit / (p.tiles * R);
+    } else {
+        constexpr int SUB = kWideRows / kUnitRows;
+        const int items = a.H_q * ((a.L_c + kWideRows - 1) / kWideRows);
+        const FcWideShape w = fc_wide_shape(R, items, S);
+        const int u = unit / SUB;
+        WideItem wi;
+        if (w.full == 0) {
+            if (u >= R * items) return false;
+            wi = wide_unit(a, valid, items, u / items, u % items);
+        } else {
+            if (u >= 8 * w.rem) return false;
+            const int j = w.full + u % w.rem;
+            wi = wide_unit(a, valid, items, j / w.per, (u / w.rem) * w.per + j % w.per);
+        }
+        if (!wi.ok) return false;
+        tile = wi.tile * SUB + unit % SUB;
+        r = wi.r;
+        h = wi.h;
+    }
+    return true;
+}
+
 // The S partials of every unit -> out and lse.  One block per unit, 8 threads per row.
 template <typename T, int D>
 __global__ __launch_bounds__(256) void attend_merge_kernel(FcAttendArgs a, FcAttendPlan p, const float* parts) {
@@ -374,30 +404,7 @@ __global__ __launch_bounds__(256) void attend_merge_kernel(FcAttendArgs a, FcAtt
     if (S == 1) return;
     const int unit = blockIdx.x;
     int tile, r, h;
-    if (p.narrow[R - 1]) {
-        if (unit >= R * a.H_q * p.tiles) return;
-        tile = unit % p.tiles;
-        r = block_of_rank(valid, (unit / p.tiles) % R);
-        h = unit / (p.tiles * R);
-    } else {
-        constexpr int SUB = kWideRows / kUnitRows;
-        const int items = a.H_q * ((a.L_c + kWideRows - 1) / kWideRows);
-        const FcWideShape w = fc_wide_shape(R, items, S);
-        const int u = unit / SUB;
-        WideItem wi;
-        if (w.full == 0) {
-            if (u >= R * items) return;
-            wi = wide_unit(a, valid, items, u / items, u % items);
-        } else {
-            if (u >= 8 * w.rem) return;
-            const int j = w.full + u % w.rem;
-            wi = wide_unit(a, valid, items, j / w.per, (u / w.rem) * w.per + j % w.per);
-        }
-        if (!wi.ok) return;
-        tile = wi.tile * SUB + unit % SUB;
-        r = wi.r;
-        h = wi.h;
-    }
+    if (!merge_unit(a, p, valid, R, S, unit, tile, r, h)) return;
     const int row = threadIdx.x >> 3, c0 = (threadIdx.x & 7) * PER;
     const int row_in_chunk = tile * kUnitRows + row;
     if (row_in_chunk >= a.L_c) return;
