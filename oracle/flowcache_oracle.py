@@ -519,7 +519,7 @@ def kv4_pack(x: np.ndarray) -> Tuple[np.ndarray, np.ndarray]:
 def kv4_values(codes: np.ndarray, scales: np.ndarray) -> np.ndarray:
     """What codes and scales stand for, ``[H, n, d]`` float64."""
     H, n, half = codes.shape
-    c = np.stack([codes & 15, codes >> 4], axis=-1).reshape(H, n, -1, 32)
+    c = np.stack([codes & 15, codes >> 4], axis=-1).reshape(H, n, half // 16, 32)
     v = np.array(KV4_MAGNITUDES + tuple(-m for m in KV4_MAGNITUDES))[c]
     s = np.where(scales == 255, np.nan, np.exp2(scales.astype(np.float64) - 127))
     return (v * s[..., None]).reshape(H, n, 2 * half)

@@ -196,3 +196,50 @@ def test_refusals():
     for kw in (dict(q=q.float()), dict(k4=None), dict(L_c=4)):
         with pytest.raises(AssertionError):
             B.flowcache_attend_kv4(**args(**kw))
+
+
+def sweep(n, seed):
+    rng = np.random.default_rng(seed)
+    for i in range(n):
+        d = int(rng.choice([64, 128]))
+        H_k = int(rng.choice([1, 2, 3, 8]))
+        H_q = H_k * int(rng.choice([1, 1, 2, 4]))
+        A = int(rng.choice([1, 2, 3, 5]))
+        L_c = int(np.exp(rng.uniform(0, np.log(700))))
+        # around the edges of 32- and 64-key tiles, and of the three tiles that K runs ahead
+        L_clean = int(rng.choice([0, 1, 64, 128, 192, 256, 320, 384])) + int(rng.integers(-2, 3)) if rng.random() < 0.6 else int(np.exp(rng.uniform(0, 9)))
+        rec = sorted(rng.choice(A, size=int(rng.integers(1, A + 1)), replace=False).tolist())
+        yield i, (H_q, H_k, d, A, L_c, max(L_clean, 0), rec), bool(rng.random() < 0.5)
+
+
+@pytest.mark.parametrize("i,shape,grow", sweep(48, 7))
+def test_sweep(i, shape, grow):
+    check(*shape, seed=i, grow=grow, reverse=bool(i & 1), new=bool(i & 2), ws=256 if i % 3 == 0 else None)
+
+
+@pytest.mark.parametrize("L_c,L_clean", [(1, 70), (40, 0), (300, 200), (520, 650)])
+def test_strided_slots(L_c, L_clean):
+    """Slots whose rows are parts of wider ones, heads with a gap: the result of contiguous ones."""
+    H, d, A = 3, 128, 2
+    q, bufs, cap4, slots = make(H, H, d, A, L_c, L_clean, 4)
+    wide = [torch.full((H, s.shape[1] + 5, d + 24), float("nan"), device=DEV, dtype=torch.bfloat16)[:, :s.shape[1], 8:8 + d] for s in slots]
+    for w, s in zip(wide, slots):
+        w.copy_(s)
+    args = (L_c, L_clean, [L_c + 2, 0], i32(0, 1), i32(2))
+    a, b = (B.flowcache_attend_kv4(q, None, None, *bufs, cap4, *c, *args) for c in (slots, wide))
+    assert torch.equal(a["out"], b["out"]) and torch.equal(a["lse"], b["lse"]) and bool(torch.isfinite(a["out"]).all())
+
+
+def test_two_calls_at_once():
+    """Two streams, a workspace each."""
+    case = (12, 12, 128, 1, 40, 9000)
+    data = [make(*case, seed) for seed in (1, 2)]
+    args = lambda x: (x[0], None, None, *x[1], x[2], *x[3], 40, 9000, [0], i32(0), i32(1))
+    want = [B.flowcache_attend_kv4(*args(x))["out"] for x in data]
+    calls = [args(x) for x in data]
+    streams = [torch.cuda.Stream() for _ in data]
+    torch.cuda.synchronize()
+    got = [[B.flowcache_attend_kv4(*c, stream=s)["out"] for c, s in zip(calls, streams)] for _ in range(5)]
+    torch.cuda.synchronize()
+    for pair in got:
+        assert all(torch.equal(x, y) for x, y in zip(pair, want))
