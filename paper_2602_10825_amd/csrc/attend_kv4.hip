@@ -196,11 +196,13 @@ __device__ __forceinline__ void attend_wide4(const FcAttendArgs& a, const FcAtte
         return __builtin_bit_cast(bf16x8_t, __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7));
     };
     auto mask_tail = [&](f32x16_t (&y)[2], int nv) {   // ragged end of a segment: keys past it
+        // (the lane's part on one side, so that the other is a constant: 32 sums were kept in registers, and others spilled for it)
+        const int mine = nv - hh * 4;
 #pragma unroll
         for (int kb = 0; kb < 2; ++kb)
 #pragma unroll
             for (int i = 0; i < 16; ++i)
-                if (kb * 32 + (i >> 2) * 8 + hh * 4 + (i & 3) >= nv) y[kb][i] = kNegBig;
+                if (kb * 32 + (i >> 2) * 8 + (i & 3) >= mine) y[kb][i] = kNegBig;
     };
     auto qk = [&](const bf16_t* Kb, f32x16_t (&y)[2]) {
 #pragma unroll
@@ -471,11 +473,13 @@ struct Narrow4Smem {
     Segments sg;
 };
 
-// The 16-byte piece of an LDS row that holds piece `piece` of the tile's row `row`: 16 neighbouring rows have 16 different banks for
-// one piece, four neighbouring ones four different pairs of banks for an aligned pair of pieces (rows of 128 bytes: two share the banks).
+// The 16-byte piece of an LDS row that holds piece `piece` of the tile's row `row`.  Rows are 256 bytes, all banks (128, half of
+// them).  For one piece of both half rows, 8 neighbouring rows have 16 different places, and so have 16 rows for one half; an
+// aligned pair of pieces of 8 neighbouring rows has 8 different pairs of places.  Row + 8 exchanges the two of a pair.
 template <int D>
 __device__ __forceinline__ int swapped(int row, int piece) {
-    return piece ^ (D == 128 ? ((row & 7) << 1) | ((row >> 3) & 1) : ((row >> 1) & 3) << 1 | ((row >> 3) & 1));
+    const int b2 = (row >> 2) & 1, b3 = (row >> 3) & 1;
+    return piece ^ (D == 128 ? ((row & 3) << 1 | (b2 << 3)) : ((row & 3) ^ b2) << 1) ^ b2 ^ b3;
 }
 
 template <int D>
@@ -532,9 +536,10 @@ __device__ __forceinline__ void attend_narrow4(const FcAttendArgs& a, const FcAt
     // scores of one tile in s, V in LDS: weights, O, l
     auto weigh = [&](f32x16_t& s, int nv) {
         if (nv < 32) {
+            const int mine = nv - hh * 4;
 #pragma unroll
             for (int i = 0; i < 16; ++i)
-                if ((i >> 2) * 8 + hh * 4 + (i & 3) >= nv) s[i] = kNegBig;
+                if ((i >> 2) * 8 + (i & 3) >= mine) s[i] = kNegBig;
         }
         float mx = s[0];
 #pragma unroll

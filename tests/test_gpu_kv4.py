@@ -12,6 +12,13 @@ DEV = "cuda"
 TORCH = {"bf16": torch.bfloat16, "f32": torch.float32}
 
 
+@pytest.fixture(scope="module", autouse=True)
+def release_memory():
+    """The blocks that these tests used go back to the device, not to the next test's torch.empty."""
+    yield
+    torch.cuda.empty_cache()
+
+
 def rows(dtype, H, n, d, seed, kind="normal"):
     rng = np.random.default_rng(seed)
     x = rng.standard_normal((H, n, d))

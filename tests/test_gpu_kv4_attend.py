@@ -14,6 +14,13 @@ pytestmark = pytest.mark.gpu
 DEV = "cuda"
 
 
+@pytest.fixture(scope="module", autouse=True)
+def release_memory():
+    """The blocks that these tests used go back to the device, not to the next test's torch.empty."""
+    yield
+    torch.cuda.empty_cache()
+
+
 def i32(*v):
     return torch.tensor(v, dtype=torch.int32, device=DEV)
 

@@ -13,6 +13,13 @@ from tests.test_gpu_kv4 import planes
 pytestmark = [pytest.mark.gpu, pytest.mark.timeout(600)]
 
 
+@pytest.fixture(scope="module", autouse=True)
+def release_memory():
+    """The blocks that these tests used go back to the device, not to the next test's torch.empty."""
+    yield
+    torch.cuda.empty_cache()
+
+
 def config(**kw):
     return RolloutConfig(**{**dict(H=2, d=64, L_c=96, n_layers=2, n_units=6, steps=8, stagger=4, budget_chunks=2, warmup_m=2, eps=0.08,
                                    obs_window=20, delta0=0.03, decay=0.8, seed=3, grid=(5, 7), kv4=True), **kw})

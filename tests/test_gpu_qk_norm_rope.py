@@ -17,6 +17,13 @@ STEP = {"bf16": 2.0 ** -8, "f32": 2.0 ** -24}
 TORCH = {"bf16": torch.bfloat16, "f32": torch.float32}
 
 
+@pytest.fixture(scope="module", autouse=True)
+def release_memory():
+    """The blocks that these tests used go back to the device, not to the next test's torch.empty."""
+    yield
+    torch.cuda.empty_cache()
+
+
 def inputs(dtype, rows, H, d, seed, scale=1.0):
     x = (np.random.default_rng(seed).standard_normal((rows, H, d)) * scale).astype(np.float32)
     return synth.to_storage(x, dtype)
