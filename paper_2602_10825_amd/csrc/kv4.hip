@@ -4,6 +4,11 @@
 namespace {
 
 constexpr int kThreads = 256;
+constexpr int kPasses = 2;             // of a packing: rows of a lane that are read before the first is worked on
+// An unpacking that writes more than this streams its output past the caches (the Infinity Cache holds 256 MB).  bf16 rows,
+// unpacked / unpacked and their importance taken, streamed against not: 250 MB 50.5 : 67.9 / 102 : 115 us, 920 MB 168 : 226 / 391 : 426,
+// 184 MB 38.7 : 39.8 / 81.7 : 80.1, 61 MB 16.8 : 18.7 / 46.4 : 44.4.
+constexpr int64_t kStreamFrom = 200ll << 20;
 
 // The largest value over the four lanes of a block (lanes 4 i .. 4 i + 3).
 __device__ __forceinline__ uint32_t quad_max(uint32_t v) {
@@ -13,74 +18,95 @@ __device__ __forceinline__ uint32_t quad_max(uint32_t v) {
     return v > o ? v : o;
 }
 
-__device__ __forceinline__ void load8(const bf16_t* p, float (&f)[8]) {
-    unpack16(*reinterpret_cast<const uint4*>(p), f, bf16_t());
-}
-__device__ __forceinline__ void load8(const float* p, float (&f)[8]) {
-    float lo[4], hi[4];
-    unpack16(reinterpret_cast<const uint4*>(p)[0], lo, 0.f);
-    unpack16(reinterpret_cast<const uint4*>(p)[1], hi, 0.f);
-#pragma unroll
-    for (int i = 0; i < 4; ++i) { f[i] = lo[i]; f[4 + i] = hi[i]; }
+// A lane has the EPL elements of one row that are 16 bytes of the cache.
+template <typename T>
+struct Lane {
+    static constexpr int EPL = Elem<T>::kVec, LPB = 32 / EPL;       // lanes per block of 32: 4 (bf16) or 8 (fp32)
+};
+template <int LPB>
+__device__ __forceinline__ uint32_t block_max(uint32_t v) {
+    v = quad_max(v);
+    if (LPB == 8) {
+        const uint32_t o = (uint32_t)__builtin_amdgcn_mov_dpp((int)v, 0x141, 0xF, 0xF, true);     // the other quad of eight
+        v = v > o ? v : o;
+    }
+    return v;
 }
 
-// A lane has 8 neighbouring elements of a row.  The scale's exponent: of the block's largest magnitude, as a float's bits, the
-// exponent less 2; less 1 from 1.75 times its power of two on, which adding a quarter to the fraction carries over.  Then the
-// largest code is 4 or 6, except that magnitudes of 1.75 2^127 and more, whose scale would make 4 an infinity, take 6 (and so
-// does everything above 1.5 2^127).  On N(0, 1) this border leaves an error of 0.1118 of a standard deviation, 2 (no exception)
-// 0.1149, 1.5 (nothing is ever cut off) 0.1154.  Packing what a packed block stands for gives the same block.
+// The scale's exponent: of the block's largest magnitude, as a float's bits, the exponent less 2; less 1 from 1.75 times its power
+// of two on, which adding a quarter to the fraction carries over.  Then the largest code is 4 or 6, except that magnitudes of
+// 1.75 2^127 and more, whose scale would make 4 an infinity, take 6 (and so does everything above 1.5 2^127).  On N(0, 1) this border
+// leaves an error of 0.1118 of a standard deviation, 2 (no exception) 0.1149, 1.5 (nothing is ever cut off) 0.1154.  Packing what a
+// packed block stands for gives the same block.
+// Bound by HBM: 24 x 128, K and V of 37440 kept rows of 74880 (460 MB read, 122 written) 107 us, 5.4 TB/s.  Read
+// past the caches (the call 245 -> 226 us with the unpacking behind it: what is read next are the packed rows); two rows a lane
+// instead of one 258 -> 245, four or eight no more.
 template <typename T, int D>
 __global__ __launch_bounds__(kThreads) void kv4_pack_kernel(FcKv4Args a) {
-    constexpr int LPR = D / 8;                       // lanes per row
+    constexpr int EPL = Lane<T>::EPL, LPB = Lane<T>::LPB, LPR = D / EPL, RPW = FC_WAVE / LPR;      // lanes per row, rows per wavefront and pass
     const int h = blockIdx.y;
     const T* src = (const T*)(blockIdx.z ? a.v_cache : a.k_cache) + h * a.head_stride;
     uint8_t* codes = (blockIdx.z ? a.v4 : a.k4) + (int64_t)h * a.capacity4 * (D / 2);
     uint8_t* scales = (blockIdx.z ? a.v4 : a.k4) + a.H_k * a.capacity4 * (D / 2) + (int64_t)h * a.capacity4 * (D / 32);
-    const int i = blockIdx.x * (kThreads / LPR) + threadIdx.x / LPR, l = threadIdx.x % LPR;
-    if (i >= a.count) return;
-    int64_t row = a.cache_pos + (int64_t)i;
-    if (a.kept) {
-        row = a.kept[(int64_t)h * a.count + i];
-        if ((uint64_t)row >= (uint64_t)a.L_k) return;        // skipped: the 4-bit row stays as it was
-    }
-    float f[8];
-    load8(src + row * a.tok_stride + 8 * l, f);
-    uint32_t top = 0;
+    const int lane = threadIdx.x & 63, l = lane % LPR;
+    const int i0 = ((blockIdx.x * (kThreads / FC_WAVE) + (threadIdx.x >> 6)) * kPasses) * RPW + lane / LPR;
+    float f[kPasses][EPL];
+    bool ok[kPasses];
 #pragma unroll
-    for (int e = 0; e < 8; ++e) {
-        const uint32_t u = __float_as_uint(f[e]) & 0x7fffffffu;
-        top = u > top ? u : top;
+    for (int e = 0; e < kPasses; ++e) {
+        const int i = i0 + e * RPW;
+        ok[e] = i < a.count;
+        int64_t row = a.cache_pos + (int64_t)(ok[e] ? i : 0);
+        if (a.kept) {
+            row = a.kept[(int64_t)h * a.count + (ok[e] ? i : 0)];
+            const bool inside = (uint64_t)row < (uint64_t)a.L_k;     // else skipped: the 4-bit row stays as it was
+            ok[e] = ok[e] && inside;
+            row = inside ? row : 0;
+        }
+        unpack16(nt_load16(reinterpret_cast<const uint4*>(src + row * a.tok_stride + EPL * l)), f[e], T());
     }
-    top = quad_max(top);
-    const bool finite = top < 0x7f800000u;
-    int byte = (int)((top + 0x200000u) >> 23) - 2;
-    byte = byte < 1 ? 1 : (byte > 252 ? 252 : byte);
-    const float s = __uint_as_float((uint32_t)byte << 23);
-    uint32_t w = 0;
-    w = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(w, f[0], f[1], s, 0);
-    w = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(w, f[2], f[3], s, 1);
-    w = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(w, f[4], f[5], s, 2);
-    w = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(w, f[6], f[7], s, 3);
-    const int64_t to = a.pos4 + (int64_t)i;
-    *reinterpret_cast<uint32_t*>(codes + to * (D / 2) + 4 * l) = finite ? w : 0u;
-    if ((l & 3) == 0) scales[to * (D / 32) + (l >> 2)] = (uint8_t)(finite ? byte : 255);
+#pragma unroll
+    for (int e = 0; e < kPasses; ++e) {
+        uint32_t top = 0;
+#pragma unroll
+        for (int k = 0; k < EPL; ++k) {
+            const uint32_t u = __float_as_uint(f[e][k]) & 0x7fffffffu;
+            top = u > top ? u : top;
+        }
+        top = block_max<LPB>(top);
+        const bool finite = top < 0x7f800000u;
+        int byte = (int)((top + 0x200000u) >> 23) - 2;
+        byte = byte < 1 ? 1 : (byte > 252 ? 252 : byte);
+        const float s = __uint_as_float((uint32_t)byte << 23);
+        byte = finite ? byte : 255;
+        uint32_t w = 0;
+        w = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(w, f[e][0], f[e][1], s, 0);
+        w = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(w, f[e][2], f[e][3], s, 1);
+        if constexpr (EPL == 8) {
+            w = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(w, f[e][4], f[e][5], s, 2);
+            w = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(w, f[e][6], f[e][7], s, 3);
+        }
+        w = finite ? w : 0u;
+        if (!ok[e]) continue;
+        const int64_t to = a.pos4 + (int64_t)(i0 + e * RPW);
+        if constexpr (EPL == 8) *reinterpret_cast<uint32_t*>(codes + to * (D / 2) + 4 * l) = w;
+        else *reinterpret_cast<uint16_t*>(codes + to * (D / 2) + 2 * l) = (uint16_t)w;
+        if (l % LPB == 0) scales[to * (D / 32) + l / LPB] = (uint8_t)byte;
+    }
 }
 
-__device__ __forceinline__ void store8(bf16_t* p, uint32_t codes, uint32_t scale) {
-    *reinterpret_cast<u32x4_native*>(p) = fc_kv4_to_bf16(codes, scale);
-}
-__device__ __forceinline__ void store8(float* p, uint32_t codes, uint32_t scale) {
+// EPL codes and their scale's byte -> 16 bytes of the cache
+__device__ __forceinline__ u32x4_native expand(uint32_t codes, uint32_t scale, bf16_t) { return fc_kv4_to_bf16(codes, scale); }
+__device__ __forceinline__ u32x4_native expand(uint32_t codes, uint32_t scale, float) {
     typedef float f32x2_t __attribute__((ext_vector_type(2)));
     const float s = __uint_as_float(scale << 23);
     const f32x2_t a = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(codes, s, 0), b = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(codes, s, 1);
-    const f32x2_t c = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(codes, s, 2), d = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(codes, s, 3);
-    reinterpret_cast<float4*>(p)[0] = make_float4(a.x, a.y, b.x, b.y);
-    reinterpret_cast<float4*>(p)[1] = make_float4(c.x, c.y, d.x, d.y);
+    return u32x4_native{__float_as_uint(a.x), __float_as_uint(a.y), __float_as_uint(b.x), __float_as_uint(b.y)};
 }
 
-template <typename T, int D>
+template <typename T, int D, bool STREAM>
 __global__ __launch_bounds__(kThreads) void kv4_unpack_kernel(FcKv4Args a) {
-    constexpr int LPR = D / 8;
+    constexpr int EPL = Lane<T>::EPL, LPB = Lane<T>::LPB, LPR = D / EPL;
     const int h = blockIdx.y;
     T* dst = (T*)(blockIdx.z ? a.v_cache : a.k_cache) + h * a.head_stride;
     const uint8_t* codes = (blockIdx.z ? a.v4 : a.k4) + (int64_t)h * a.capacity4 * (D / 2);
@@ -88,18 +114,26 @@ __global__ __launch_bounds__(kThreads) void kv4_unpack_kernel(FcKv4Args a) {
     const int i = blockIdx.x * (kThreads / LPR) + threadIdx.x / LPR, l = threadIdx.x % LPR;
     if (i >= a.count) return;
     const int64_t from = a.pos4 + (int64_t)i;
-    store8(dst + (a.cache_pos + (int64_t)i) * a.tok_stride + 8 * l, *reinterpret_cast<const uint32_t*>(codes + from * (D / 2) + 4 * l),
-           scales[from * (D / 32) + (l >> 2)]);
+    uint32_t w;
+    if constexpr (EPL == 8) w = *reinterpret_cast<const uint32_t*>(codes + from * (D / 2) + 4 * l);
+    else w = *reinterpret_cast<const uint16_t*>(codes + from * (D / 2) + 2 * l);
+    const u32x4_native v = expand(w, scales[from * (D / 32) + l / LPB], T());
+    u32x4_native* to = reinterpret_cast<u32x4_native*>(dst + (a.cache_pos + (int64_t)i) * a.tok_stride + EPL * l);
+    if constexpr (STREAM) __builtin_nontemporal_store(v, to);
+    else *to = v;
 }
 
 template <typename T, int D>
 int launch(const FcKv4Args& a, bool pack, hipStream_t s) {
-    const int rows = kThreads / (D / 8);
-    const dim3 grid((a.count + rows - 1) / rows, a.H_k, a.v_cache ? 2 : 1);
+    const int64_t rows = kThreads / (D / Lane<T>::EPL) * (pack ? kPasses : 1);
+    const dim3 grid((unsigned)((a.count + rows - 1) / rows), a.H_k, a.v_cache ? 2 : 1);
+    const int64_t written = (int64_t)a.count * a.H_k * D * sizeof(T) * (a.v_cache ? 2 : 1);
     if (pack)
         kv4_pack_kernel<T, D><<<grid, kThreads, 0, s>>>(a);
+    else if (written > kStreamFrom)
+        kv4_unpack_kernel<T, D, true><<<grid, kThreads, 0, s>>>(a);
     else
-        kv4_unpack_kernel<T, D><<<grid, kThreads, 0, s>>>(a);
+        kv4_unpack_kernel<T, D, false><<<grid, kThreads, 0, s>>>(a);
     FC_LAUNCH_CHECK();
     return FC_OK;
 }
