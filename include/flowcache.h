@@ -377,7 +377,8 @@ size_t flowcache_kv_compress_status_offset(int H_k, int L_k, int d, int budget, 
  *   k, v     [dev] the same with H_k heads and kv_new_tok_stride.  So all three may be parts of one
  *                  fused projection's rows.  v may be NULL: then V is not written
  *   q_weight,
- *   k_weight [dev] [d] float32, NULL = ones (read only if norm != 0)
+ *   k_weight [dev] [d] float32, NULL = ones (read only if norm != 0).  With norm_eps = 0 a head of
+ *                  zeros gives NaN
  *   dims     [host] [3] even, >= 0, their sum <= d;   frame0 [host] [A]
  *   pairing  FC_ROPE_INTERLEAVED: pair p is elements (2 p, 2 p + 1);  FC_ROPE_HALVES: (p, d / 2 + p)
  *   q_out    [dev] [A*L_c, H_q, d] compact, as flowcache_attend takes it; may be q where q's rows follow
@@ -387,7 +388,7 @@ size_t flowcache_kv_compress_status_offset(int H_k, int L_k, int d, int budget, 
  *                  values go to slot active_off[recompute_idx[r]]; nothing else in the caches is touched
  * flowcache_attend follows with k_new = v_new = NULL.  q, k and v must not overlap what is written
  * (but for q_out = q).
- * Errors: null pointers, grid_h or grid_w < 1, theta <= 0 or not finite, norm_eps < 0 or not finite,
+ * Errors: null pointers, grid_h or grid_w < 1, theta < 1 or not finite, norm_eps < 0 or not finite,
  * dims odd, negative or beyond d, slots outside the cache or overlapping -> FC_INVALID_ARGUMENT; d not in
  * {64, 128}, strides or pointers that are not multiples of 16 bytes -> FC_UNSUPPORTED.
  */
@@ -444,8 +445,10 @@ int flowcache_kv4_unpack(const void* k4, const void* v4, int capacity4, int pos4
  * k4 / v4 (as above, written by flowcache_kv4_pack) and the slots of active chunks 0..c, which alone lie
  * in k_cache / v_cache: active_off may start at 0.  Arguments, errors and workspace as there, and
  *
- *   k4, v4   [dev] buffers of capacity4 rows per head; may be NULL if L_clean = 0
- *   dtype    FC_BF16 (type of q, the caches and out); FC_F32 -> FC_UNSUPPORTED.  The 4-bit values are
+ *   k4, v4   [dev] buffers of capacity4 rows per head; may be NULL if L_clean = 0.  What the rows that
+ *                  are seen stand for has to be finite, as the caches' elements have to be
+ *   dtype    FC_BF16 (type of q, the caches and out); FC_F32 -> FC_UNSUPPORTED, and so are more than
+ *            2^31 - 257 visible positions.  The 4-bit values are
  *            bf16 operands without rounding, so the result is flowcache_attend's on the unpacked rows
  * The importance mass is not emitted here: at a commit the clean keys are unpacked for the selection
  * anyway, and flowcache_attention_mass takes them from there.

@@ -40,7 +40,7 @@ const char* flowcache_status_string(int status) {
     }
 }
 
-int flowcache_version(void) { return 100; }
+int flowcache_version(void) { return 101; }
 
 // ------------------------------------------------------------------ chunk_decide
 size_t flowcache_chunk_decide_workspace(int A, int64_t chunk_elems) {
@@ -283,7 +283,7 @@ int flowcache_qk_norm_rope(const void* q, int64_t q_tok_stride, const void* k, c
     if (st != FC_OK) return st;
     st = check_slots(A, L_c, L_clean, capacity, active_off);
     if (st != FC_OK) return st;
-    if (grid_h < 1 || grid_w < 1 || !(theta > 0.0) || !std::isfinite(theta)) return FC_INVALID_ARGUMENT;
+    if (grid_h < 1 || grid_w < 1 || !(theta >= 1.0) || !std::isfinite(theta)) return FC_INVALID_ARGUMENT;
     if (norm && (!(norm_eps >= 0.f) || !std::isfinite(norm_eps))) return FC_INVALID_ARGUMENT;
     if (pairing != FC_ROPE_INTERLEAVED && pairing != FC_ROPE_HALVES) return FC_INVALID_ARGUMENT;
     int64_t sum = 0;
@@ -303,7 +303,7 @@ int flowcache_qk_norm_rope(const void* q, int64_t q_tok_stride, const void* k, c
     a.q_out = q_out; a.k_cache = k_cache; a.v_cache = v_cache;
     a.head_stride = kv_head_stride; a.tok_stride = kv_tok_stride;
     a.dtype = dtype; a.H_q = H_q; a.H_k = H_k; a.d = d; a.L_c = L_c; a.A = A;
-    a.q_weight = q_weight; a.k_weight = k_weight; a.eps = norm_eps; a.norm = norm; a.pairing = pairing;
+    a.q_weight = norm ? q_weight : nullptr; a.k_weight = norm ? k_weight : nullptr; a.eps = norm_eps; a.norm = norm; a.pairing = pairing;
     a.grid_h = grid_h; a.grid_w = grid_w;
     a.pairs_t = dims[0] / 2; a.pairs_th = (dims[0] + dims[1]) / 2;
     // theta^(-2 i / dims) by repeated products: at most 64 roundings to 64 bits instead of as many powers (3 us of a call)
@@ -382,7 +382,7 @@ int flowcache_attend_kv4(const void* q, const void* k_new, const void* v_new, co
     if (st != FC_OK) return st;
     if (H_q % H_k != 0) return FC_INVALID_ARGUMENT;
     if (!(softmax_scale >= 0.f) || !std::isfinite(softmax_scale)) return FC_INVALID_ARGUMENT;
-    if (dtype != FC_BF16 || (int64_t)A * L_c > INT32_MAX || (int64_t)L_clean + (int64_t)A * L_c > INT32_MAX) return FC_UNSUPPORTED;
+    if (dtype != FC_BF16 || (int64_t)L_clean + (int64_t)A * L_c > INT32_MAX - 256) return FC_UNSUPPORTED;   // (kernels round up to tiles)
     st = check_slots(A, L_c, 0, capacity, active_off);
     if (st != FC_OK) return st;
     if (!aligned16(q) || !aligned16(out) || (k_new && (!aligned16(k_new) || !aligned16(v_new))) ||

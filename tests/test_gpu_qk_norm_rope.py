@@ -159,9 +159,21 @@ def test_queries_in_place_and_a_second_stream():
     caches = [torch.zeros(4, 66, 64, device=DEV, dtype=torch.bfloat16) for _ in range(2)]
     i32 = lambda *v: torch.tensor(v, dtype=torch.int32, device=DEV)
     args = (66, 0, [0], i32(0), i32(1), (24, 20, 20), (5, 5), [3])
-    want = B.flowcache_qk_norm_rope(q, k, k, *caches, *args)
-    got = B.flowcache_qk_norm_rope(q, k, k, *caches, *args, q_out=q)
-    assert got is q and torch.equal(got, want)
+    for pairing in ("interleaved", "halves"):
+        want = B.flowcache_qk_norm_rope(q, k, k, *caches, *args, pairing=pairing)
+        same = q.clone()
+        got = B.flowcache_qk_norm_rope(same, k, k, *caches, *args, pairing=pairing, q_out=same)
+        assert got is same and torch.equal(got, want) and not torch.equal(got, q)
+
+
+def test_without_a_norm_the_weights_are_not_read():
+    q = torch.randn(5, 2, 64, device=DEV)
+    cache = torch.zeros(2, 5, 64, device=DEV)
+    i32 = lambda *v: torch.tensor(v, dtype=torch.int32, device=DEV)
+    w = torch.full((64,), float("nan"), device=DEV)
+    args = (q, q, None, cache, None, 5, 0, [0], i32(0), i32(1), (24, 20, 20), (2, 2), [9])
+    a, b = (B.flowcache_qk_norm_rope(*args, q_weight=x, k_weight=x, norm_eps=None) for x in (None, w))
+    assert torch.equal(a, b) and bool(torch.isfinite(cache).all())
 
 
 def test_many_tokens_of_many_heads():

@@ -128,7 +128,7 @@ def test_qk_norm_rope_rejects_bad_arguments(L):
     assert rope(L, d=96) == UNSUPPORTED
     assert rope(L, gh=0) == INVALID and rope(L, gw=-3) == INVALID
     assert rope(L, gh=1 << 20, gw=1 << 20) == UNSUPPORTED
-    for theta in (0.0, -1.0, math.inf, math.nan):
+    for theta in (0.0, -1.0, 0.99, math.inf, math.nan):
         assert rope(L, theta=theta) == INVALID
     for eps in (-1e-6, math.inf, math.nan):
         assert rope(L, eps=eps) == INVALID
@@ -198,5 +198,6 @@ def test_attend_kv4_rejects_bad_arguments(L):
     for name in ("q", "k_new", "v_new", "k4", "v4", "kc", "vc", "out"):
         assert attend(**{name: ctypes.c_void_p(0x10004)}) == UNSUPPORTED, name
     assert attend(L_clean=2 ** 31 - 200, cap4=2 ** 31 - 1) == UNSUPPORTED  # positions beyond 32 bits
+    assert attend(L_clean=2 ** 31 - 256 - 256, cap4=2 ** 31 - 1) == UNSUPPORTED     # or so near that a tile passes them
     assert L.flowcache_attend_kv4_workspace(2, 128, 4, 64) == L.flowcache_attend_workspace(2, 128, 4, 1, 64, 0, 50)
     assert L.flowcache_attend_kv4_workspace(0, 128, 4, 64) == 0 and L.flowcache_attend_kv4_workspace(2, 128, 4, 96) == 0
