@@ -579,7 +579,7 @@ def flowcache_attend_kv4(q: torch.Tensor, k_new: Optional[torch.Tensor], v_new: 
                          softmax_scale: float = 0.0, out: Optional[torch.Tensor] = None, want_lse: bool = True,
                          workspace: Optional[torch.Tensor] = None, stream=None) -> Dict[str, Optional[torch.Tensor]]:
     """:func:`flowcache_attend` with the clean region in the 4-bit buffers k4 / v4; the caches ``[H_k, capacity, d]``
-    (bfloat16) hold the active chunks' slots alone.  k4 and v4 may be None if ``L_clean`` is 0."""
+    hold the active chunks' slots alone.  k4 and v4 may be None if ``L_clean`` is 0."""
     call = "flowcache_attend_kv4"
     rows, H_q, d = q.shape
     H_k, capacity, _ = k_cache.shape

@@ -14,7 +14,7 @@ ROOT = os.path.dirname(HERE)
 CSRC = os.path.join(HERE, "csrc")
 OBJ = os.path.join(HERE, "_build")
 LIB = os.path.join(HERE, "libflowcache.so")
-SOURCES = ["api.hip", "decide.hip", "attend_f32.hip", "attend_bf16.hip", "attend_kv4.hip", "mass.hip",
+SOURCES = ["api.hip", "decide.hip", "attend_f32.hip", "attend_bf16.hip", "attend_kv4.hip", "attend_kv4_f32.hip", "mass.hip",
            "compress.hip", "residual.hip", "rope.hip", "kv4.hip", "sched.cpp"]
 HIPCC = os.environ.get("HIPCC", "/opt/rocm/bin/hipcc")
 FLAGS = ["--offload-arch=gfx950", "-O3", "-std=c++17", "-fPIC", "-fvisibility=hidden",
@@ -23,7 +23,7 @@ FLAGS = ["--offload-arch=gfx950", "-O3", "-std=c++17", "-fPIC", "-fvisibility=hi
 # The attention kernels' inputs are finite by contract and they may assume so (cheaper max);
 # every file that CHECKS arguments for NaN (api.hip) or writes NaN on purpose (decide, mass) is
 # compiled with full NaN semantics.
-NO_NAN_OK = {"attend_bf16.hip", "attend_f32.hip", "attend_kv4.hip"}
+NO_NAN_OK = {"attend_bf16.hip", "attend_f32.hip", "attend_kv4.hip", "attend_kv4_f32.hip"}
 
 
 def _compile(src: str) -> str:

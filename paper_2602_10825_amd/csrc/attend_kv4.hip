@@ -5,7 +5,7 @@
 // In these kernels FcAttendArgs describes the slots alone (its L_clean is 0); the clean region, x.L_clean rows of the 4-bit
 // buffers, comes first in the order of the key tiles and never shares a tile with a slot.
 #include "attend_bf16.hpp"
-#include "kv4.hpp"
+#include "kv4_tiles.hpp"
 
 namespace {
 
@@ -473,15 +473,6 @@ struct Narrow4Smem {
     Segments sg;
 };
 
-// The 16-byte piece of an LDS row that holds piece `piece` of the tile's row `row`.  Rows are 256 bytes, all banks (128, half of
-// them).  For one piece of both half rows, 8 neighbouring rows have 16 different places, and so have 16 rows for one half; an
-// aligned pair of pieces of 8 neighbouring rows has 8 different pairs of places.  Row + 8 exchanges the two of a pair.
-template <int D>
-__device__ __forceinline__ int swapped(int row, int piece) {
-    const int b2 = (row >> 2) & 1, b3 = (row >> 3) & 1;
-    return piece ^ (D == 128 ? ((row & 3) << 1 | (b2 << 3)) : ((row & 3) ^ b2) << 1) ^ b2 ^ b3;
-}
-
 template <int D>
 __device__ __forceinline__ void attend_narrow4(const FcAttendArgs& a, const FcAttendPlan& p, uint32_t valid,
                                                Narrow4Smem<D>& sm, float* parts, const FcKv4& x) {
@@ -490,7 +481,6 @@ __device__ __forceinline__ void attend_narrow4(const FcAttendArgs& a, const FcAt
     constexpr int OROW = Narrow4Smem<D>::OROW;
     constexpr int VPR = D / 8;           // 16-byte vectors per row
     constexpr int LD = 32 * VPR / FC_WAVE;
-    constexpr int W4 = D / 64;           // 16-byte vectors of codes in half a row, each with a scale of its own
     constexpr float kSlack = 8.0f;       // the exponents' reference follows the row maximum at this distance (log2)
     Segments& sg = sm.sg;
     float *m_s = sm.m_s, *l_s = sm.l_s;
@@ -531,7 +521,7 @@ __device__ __forceinline__ void attend_narrow4(const FcAttendArgs& a, const FcAt
     // transposing reads of V: the lane's key row of the first 4-key patch, and its piece there; what depends on the patch and
     // on the block of the value dimension is exchanged into it
     const int l16 = lane & 15, v_row = hh * 4 + (l16 >> 2);
-    const int v_at = v_row * D + swapped<D>(v_row, ((lane >> 4) & 1) * 2 + ((l16 & 3) >> 1)) * 8 + (l16 & 1) * 4;
+    const int v_at = v_row * D + fc_swapped<D>(v_row, ((lane >> 4) & 1) * 2 + ((l16 & 3) >> 1)) * 8 + (l16 & 1) * 4;
 
     // scores of one tile in s, V in LDS: weights, O, l
     auto weigh = [&](f32x16_t& s, int nv) {
@@ -585,53 +575,28 @@ __device__ __forceinline__ void attend_narrow4(const FcAttendArgs& a, const FcAt
             }
     };
 
-    // ---- tiles of codes: half a row of K and of V per lane, with W4 scales each
-    struct Codes { u32x4_native k[W4], v[W4]; uint32_t ks, vs; };
-    const uint8_t *k4 = x.k + (int64_t)hk * x.head_codes, *v4 = x.v + (int64_t)hk * x.head_codes;
-    const int64_t to_scales = x.scales_at + (int64_t)hk * (x.head_scales - x.head_codes);
-    auto fetch4 = [&](Codes& c, int tt) {
-        tt = tt < tiles4 ? tt : tiles4 - 1;              // (past the end: fetched again, never used)
-        const int left = x.L_clean - tt * 32 - 1;
-        const uint32_t row = (uint32_t)(l32 < left ? l32 : left);
-        const uint8_t *kt = k4 + (int64_t)tt * (16 * D), *vt = v4 + (int64_t)tt * (16 * D);
-        const uint8_t *ks = k4 + to_scales + (int64_t)tt * D, *vs = v4 + to_scales + (int64_t)tt * D;
-#pragma unroll
-        for (int i = 0; i < W4; ++i) {
-            c.k[i] = *reinterpret_cast<const u32x4_native*>(kt + (row * (D / 2) + hh * (D / 4) + 16 * i));
-            c.v[i] = *reinterpret_cast<const u32x4_native*>(vt + (row * (D / 2) + hh * (D / 4) + 16 * i));
-        }
-        const uint32_t at = row * (D / 32) + hh * W4;
-        if constexpr (W4 == 2) {
-            c.ks = *reinterpret_cast<const uint16_t*>(ks + at);
-            c.vs = *reinterpret_cast<const uint16_t*>(vs + at);
-        } else {
-            c.ks = ks[at];
-            c.vs = vs[at];
-        }
-    };
-    const int st_row = l32 * D, st_swap = swapped<D>(l32, hh * (D / 16)) * 8;
-    auto codes_tile = [&](Codes& c, int tt) {
+    // ---- tiles of codes
+    const FcCodesHead head{x.k + (int64_t)hk * x.head_codes, x.v + (int64_t)hk * x.head_codes,
+                           x.scales_at + (int64_t)hk * (x.head_scales - x.head_codes), x.L_clean, tiles4};
+    const int st_row = l32 * D, st_swap = fc_swapped<D>(l32, hh * (D / 16)) * 8;
+    auto codes_tile = [&](FcCodes<D>& c, int tt) {
         f32x16_t s;
 #pragma unroll
         for (int i = 0; i < 16; ++i) s[i] = 0.f;
 #pragma unroll
-        for (int st = 0; st < KS; ++st) {
-            const u32x4_native kf = fc_kv4_to_bf16(c.k[st >> 2][st & 3], W4 == 1 ? c.ks : (c.ks >> (8 * (st >> 2))) & 255u);
-            s = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8_t, kf), qf[st], s, 0, 0, 0);
-        }
+        for (int st = 0; st < KS; ++st)
+            s = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8_t, c.key(st)), qf[st], s, 0, 0, 0);
         // the wavefront's own tile: its LDS accesses are served in order, no barrier is needed
 #pragma unroll
-        for (int st = 0; st < KS; ++st)
-            *reinterpret_cast<u32x4_native*>(&vw[st_row + (st_swap ^ (st * 8))]) =
-                fc_kv4_to_bf16(c.v[st >> 2][st & 3], W4 == 1 ? c.vs : (c.vs >> (8 * (st >> 2))) & 255u);
+        for (int st = 0; st < KS; ++st) *reinterpret_cast<u32x4_native*>(&vw[st_row + (st_swap ^ (st * 8))]) = c.value(st);
         const int nv = x.L_clean - tt * 32 < 32 ? x.L_clean - tt * 32 : 32;
-        fetch4(c, tt + 2 * kSplitWaves);
+        c.fetch(head, tt + 2 * kSplitWaves, l32, hh);
         weigh(s, nv);
     };
     if (t < t_end4) {
-        Codes c0, c1;
-        fetch4(c0, t);
-        fetch4(c1, t + kSplitWaves);
+        FcCodes<D> c0, c1;
+        c0.fetch(head, t, l32, hh);
+        c1.fetch(head, t + kSplitWaves, l32, hh);
         for (;;) {
             codes_tile(c0, t);
             t += kSplitWaves;
@@ -672,7 +637,7 @@ __device__ __forceinline__ void attend_narrow4(const FcAttendArgs& a, const FcAt
     while (t < t_end) {
 #pragma unroll
         for (int i = 0; i < LD; ++i) {
-            const int row = i * (FC_WAVE / VPR) + ld_row, at = row * D + swapped<D>(row, ld_col) * 8;
+            const int row = i * (FC_WAVE / VPR) + ld_row, at = row * D + fc_swapped<D>(row, ld_col) * 8;
             *reinterpret_cast<u32x4_native*>(&kw[at]) = kr[i];
             *reinterpret_cast<u32x4_native*>(&vw[at]) = vr[i];
         }
@@ -701,59 +666,6 @@ __device__ __forceinline__ void attend_narrow4(const FcAttendArgs& a, const FcAt
                 f32x4_t{o[b][4 * g], o[b][4 * g + 1], o[b][4 * g + 2], o[b][4 * g + 3]};
     __syncthreads();
     finish_unit<bf16_t, D, OROW>(a, p, it, sm.o, m_s, l_s, parts);
-}
-
-// The S <= MOST partials of every 32-row unit -> out and lse, as attend_merge_kernel does it but for few rows: a thread has four
-// columns of one row, the factors of a row are computed once, and all of a row's partials are asked for at once, before those
-// (12 x 128, one row on 61201 keys in 20 ranges 15.2 -> 6.4 us; 256 rows on 49201 in 20 ranges 17.9 -> 10.6).
-constexpr int kMergeThreads = 256;
-template <int D>
-struct MergeShape {
-    static constexpr int TPR = D / 4, RPB = kMergeThreads / TPR, BPU = kUnitRows / RPB;   // threads per row, rows per block, blocks per unit
-};
-template <int D, int MOST>
-__global__ __launch_bounds__(kMergeThreads) void merge4_kernel(FcAttendArgs a, FcAttendPlan p, const float* parts) {
-    constexpr int TPR = MergeShape<D>::TPR, RPB = MergeShape<D>::RPB, BPU = MergeShape<D>::BPU;
-    __shared__ float m_s[MOST][RPB], l_s[MOST][RPB];
-    const uint32_t valid = valid_blocks(a);
-    const int R = __popc(valid);
-    if (R == 0) return;
-    const int S = p.splits[R - 1];
-    if (S == 1) return;
-    const int unit = blockIdx.x / BPU, row0 = blockIdx.x % BPU * RPB;
-    int tile, r, h;
-    if (!merge_unit(a, p, valid, R, S, unit, tile, r, h)) return;
-    const int first_row = tile * kUnitRows + row0;
-    if (first_row >= a.L_c) return;
-    const int row = threadIdx.x / TPR, c0 = threadIdx.x % TPR * 4;
-    const float4* src = reinterpret_cast<const float4*>(parts + ((int64_t)unit * S * kUnitRows + row0 + row) * D + c0);
-    float4 v[MOST];
-#pragma unroll
-    for (int s = 0; s < MOST; ++s) v[s] = src[(int64_t)(s < S ? s : S - 1) * (kUnitRows * D / 4)];
-    const float* ml = parts + (int64_t)p.parts * kUnitRows * D + (int64_t)unit * S * 2 * kUnitRows + row0;
-    for (int i = threadIdx.x; i < S * RPB; i += kMergeThreads) {
-        m_s[i / RPB][i % RPB] = ml[i / RPB * 2 * kUnitRows + i % RPB];
-        l_s[i / RPB][i % RPB] = ml[(i / RPB * 2 + 1) * kUnitRows + i % RPB];
-    }
-    __syncthreads();
-    float mt = kNegBig;
-#pragma unroll
-    for (int s = 0; s < MOST; ++s) mt = fmaxf(mt, s < S ? m_s[s][row] : kNegBig);
-    float acc[4] = {0.f, 0.f, 0.f, 0.f}, l = 0.f;
-#pragma unroll
-    for (int s = 0; s < MOST; ++s) {
-        const float f = s < S ? __builtin_amdgcn_exp2f(m_s[s][row] - mt) : 0.f;
-        l = fmaf(s < S ? l_s[s][row] : 0.f, f, l);
-        acc[0] = fmaf(v[s].x, f, acc[0]);
-        acc[1] = fmaf(v[s].y, f, acc[1]);
-        acc[2] = fmaf(v[s].z, f, acc[2]);
-        acc[3] = fmaf(v[s].w, f, acc[3]);
-    }
-    if (first_row + row >= a.L_c) return;
-    const float inv = 1.0f / l;
-    const int64_t grow = (int64_t)r * a.L_c + first_row + row;
-    store_out((bf16_t*)a.out + (grow * a.H_q + h) * D + c0, acc[0] * inv, acc[1] * inv, acc[2] * inv, acc[3] * inv);
-    if (a.lse && c0 == 0) a.lse[(int64_t)h * a.A * a.L_c + grow] = (mt + __builtin_amdgcn_logf(l)) * 0.6931471805599453f;
 }
 
 // WIDE and NARROW say which of the two bodies some recompute count of this launch asks for.
@@ -796,16 +708,7 @@ int launch_kv4(FcAttendArgs a, const FcKv4& x, hipStream_t s) {
     else
         attend_kv4_kernel<D, true, true><<<p.grid, NT, 0, s>>>(a, p, (float*)a.ws, x);
     FC_LAUNCH_CHECK();
-    if (p.merge_grid > 0) {
-        const dim3 grid(p.merge_grid * MergeShape<D>::BPU);
-        int most = 1;
-        for (int R = 0; R < a.A; ++R) most = p.splits[R] > most ? p.splits[R] : most;
-        if (most <= 4) merge4_kernel<D, 4><<<grid, kMergeThreads, 0, s>>>(a, p, (const float*)a.ws);
-        else if (most <= 12) merge4_kernel<D, 12><<<grid, kMergeThreads, 0, s>>>(a, p, (const float*)a.ws);
-        else merge4_kernel<D, kMaxSplits><<<grid, kMergeThreads, 0, s>>>(a, p, (const float*)a.ws);
-        FC_LAUNCH_CHECK();
-    }
-    return FC_OK;
+    return launch_merge4<bf16_t, D>(a, p, s);
 }
 
 }  // namespace

@@ -128,6 +128,7 @@ int fc_launch_attend_bf16(const FcAttendArgs& a, hipStream_t s);
 // K or V rows in 4 bits (kv4.hpp), head by head: codes, then (from byte scales_at on) scales.
 struct FcKv4 { const uint8_t* k; const uint8_t* v; int64_t head_codes, head_scales, scales_at; int L_clean; };
 int fc_launch_attend_kv4(const FcAttendArgs& a, const FcKv4& x, hipStream_t s);
+int fc_launch_attend_kv4_f32(const FcAttendArgs& a, const FcKv4& x, hipStream_t s);
 
 struct FcKv4Args {
     void* k_cache; void* v_cache; int64_t head_stride, tok_stride; fc_dtype dtype; int H_k, d, L_k;

@@ -2,7 +2,11 @@
 
 Tolerance.  A weight is rounded to bf16, half a step of 2^-8, and so is its share of the row's sum: the row is off by at most
 2^-8 (sum p |v| + |out|) <= 2^-7 sum p |v|.  Scores, exponentials and sums in fp32 add about 2^-16 of that: 2^-13.  Then the output's rounding,
-2^-8 |out|.  The logarithm of the sum: 2^-8 for the weights, 1e-5 for the rest."""
+2^-8 |out|.  The logarithm of the sum: 2^-8 for the weights, 1e-5 for the rest.
+
+fp32, in units of 2^-24.  A score is 24 (a slot's key 48) additions of products that are exact to 1: 48 B, B the largest sum of
+|q k| times the scale that the row sees; twice that for weight and sum.  Exponential, weight's parts and reference 16.  The row's sums over the
+tiles of one wavefront, 12 additions each of 32 keys, and the merge of 8 wavefronts and up to 32 ranges 40: all times sum p |v|."""
 import numpy as np
 import pytest
 import torch
@@ -25,17 +29,17 @@ def i32(*v):
     return torch.tensor(v, dtype=torch.int32, device=DEV)
 
 
-def make(H_q, H_k, d, A, L_c, L_clean, seed, spare=9, grow=False):
+def make(H_q, H_k, d, A, L_c, L_clean, seed, spare=9, grow=False, dtype=torch.bfloat16):
     g = torch.Generator(device=DEV)
     g.manual_seed(seed)
     n = lambda *s: torch.randn(s, generator=g, device=DEV)
-    q = n(A * L_c, H_q, d).to(torch.bfloat16)
+    q = n(A * L_c, H_q, d).to(dtype)
     clean = [n(H_k, max(L_clean, 1), d) for _ in range(2)]
     slots = [n(H_k, A * L_c + 16, d) for _ in range(2)]
     if grow:                                            # scores that grow along the keys: the reference is raised again and again
         clean[0] *= torch.linspace(0.05, 4, max(L_clean, 1), device=DEV)[None, :, None]
         slots[0] *= torch.linspace(3, 6, A * L_c + 16, device=DEV)[None, :, None]
-    clean, slots = [x.to(torch.bfloat16) for x in clean], [x.to(torch.bfloat16) for x in slots]
+    clean, slots = [x.to(torch.bfloat16) for x in clean], [x.to(dtype) for x in slots]
     cap4 = L_clean + spare
     bufs = []
     for x in clean:
@@ -51,10 +55,10 @@ def make(H_q, H_k, d, A, L_c, L_clean, seed, spare=9, grow=False):
 
 
 def reference(q, values, slots, off, L_c, rec, scale):
-    """(out, its tolerance, log sum exp) of the listed row blocks, [rows, H_q, d] and [H_q, rows]"""
+    """(out, its tolerance, log sum exp and its tolerance) of the listed row blocks, [rows, H_q, d] and [H_q, rows]"""
     H_q, d = q.shape[1:]
     H_k = slots[0].shape[0]
-    out, tol, lse = [], [], []
+    out, tol, lse, lse_tol = [], [], [], []
     for r, c in enumerate(rec):
         k, v = (torch.cat([x] + [s[:, o:o + L_c].double() for o in off[:c + 1]], 1) for x, s in zip(values, slots))
         k, v = (x.repeat_interleave(H_q // H_k, 0) for x in (k, v))
@@ -62,13 +66,23 @@ def reference(q, values, slots, off, L_c, rec, scale):
         p = torch.softmax(s, -1)
         o = p @ v
         out.append(o.transpose(0, 1))
-        tol.append((2.0 ** -8 * o.abs() + (2.0 ** -7 + 2.0 ** -13) * (p @ v.abs())).transpose(0, 1))
+        if q.dtype == torch.bfloat16:
+            t = 2.0 ** -8 * o.abs() + (2.0 ** -7 + 2.0 ** -13) * (p @ v.abs())
+            t_lse = torch.full_like(s[..., 0], 2.0 ** -8 + 1e-5)
+        else:
+            row = (q[r * L_c:(r + 1) * L_c].double().abs().transpose(0, 1) @ k.abs().transpose(1, 2).contiguous()).amax(-1) * scale
+            u = 2.0 ** -24 * (2 * 48 * row + 16 + 40 + 12 * (s.shape[-1] / 256 + 1))
+            t = 2.0 ** -24 * o.abs() + u[..., None] * (p @ v.abs())
+            t_lse = u + 2.0 ** -23 * torch.logsumexp(s, -1).abs()
+        tol.append(t.transpose(0, 1))
         lse.append(torch.logsumexp(s, -1))
-    return torch.cat(out), torch.cat(tol), torch.cat(lse, 1)
+        lse_tol.append(t_lse)
+    return torch.cat(out), torch.cat(tol), torch.cat(lse, 1), torch.cat(lse_tol, 1)
 
 
-def check(H_q, H_k, d, A, L_c, L_clean, rec, seed=0, scale=0.0, reverse=False, grow=False, new=False, ws=None, idx=None, n=None, stream=None):
-    q, bufs, cap4, slots = make(H_q, H_k, d, A, L_c, L_clean, seed, grow=grow)
+def check(H_q, H_k, d, A, L_c, L_clean, rec, seed=0, scale=0.0, reverse=False, grow=False, new=False, ws=None, idx=None, n=None, stream=None,
+          dtype=torch.bfloat16):
+    q, bufs, cap4, slots = make(H_q, H_k, d, A, L_c, L_clean, seed, grow=grow, dtype=dtype)
     off = [3 + i * L_c for i in range(A)]
     if reverse:
         off.reverse()
@@ -77,7 +91,7 @@ def check(H_q, H_k, d, A, L_c, L_clean, rec, seed=0, scale=0.0, reverse=False, g
     values = [x[:, :L_clean].double() for x in values]
     kn = vn = None
     if new:
-        kn, vn = (torch.randn((A * L_c, H_k, d), device=DEV).to(torch.bfloat16) for _ in range(2))
+        kn, vn = (torch.randn((A * L_c, H_k, d), device=DEV).to(dtype) for _ in range(2))
     out = torch.full_like(q, 7.0)
     t_idx, t_n = i32(*(list(rec) + [-1] * (A - len(rec)) if idx is None else idx)), i32(len(rec) if n is None else n)
     if ws is not None:
@@ -92,10 +106,13 @@ def check(H_q, H_k, d, A, L_c, L_clean, rec, seed=0, scale=0.0, reverse=False, g
                 assert torch.equal(s[:, off[c]:off[c] + L_c], x[r * L_c:(r + 1) * L_c].transpose(0, 1))
     rows = len(rec) * L_c
     if rows:
-        ref, tol, lse = reference(q, values, slots, off, L_c, rec, scale or d ** -0.5)
-        err = (got["out"][:rows].double() - ref).abs() - tol
-        assert float(err.max()) <= 0, (float(err.max()), float(tol.max()))
-        assert float((got["lse"][:, :rows].double() - lse).abs().max()) <= 2.0 ** -8 + 1e-5
+        ref, tol, lse, lse_tol = reference(q, values, slots, off, L_c, rec, scale or d ** -0.5)
+        err = (got["out"][:rows].double() - ref).abs()
+        assert float((err - tol).max()) <= 0, (float(err.max()), float(tol.max()))
+        assert float(((got["lse"][:, :rows].double() - lse).abs() - lse_tol).max()) <= 0
+        if dtype == torch.float32 and not grow:             # the library's bar for fp32 attention
+            assert float(err.max() / ref.abs().max()) <= 1e-5
+            assert float((err.norm(dim=-1) / ref.norm(dim=-1)).max()) <= 1e-5
     assert bool((out[rows:] == 7).all())
     return got["out"]
 
@@ -109,17 +126,19 @@ def check(H_q, H_k, d, A, L_c, L_clean, rec, seed=0, scale=0.0, reverse=False, g
     (96, 8, 64, 1, 300, 700, [0]), (1, 1, 128, 1, 64, 20011, [0]), (64, 8, 128, 2, 520, 100, [0, 1]),
 ])
 @pytest.mark.parametrize("form", ["plain", "grow", "other"])
-def test_matches_float64(H_q, H_k, d, A, L_c, L_clean, rec, form):
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32])
+def test_matches_float64(H_q, H_k, d, A, L_c, L_clean, rec, form, dtype):
     if form == "other":                                 # slots in reverse, new rows, a scale, no room to divide the keys
-        check(H_q, H_k, d, A, L_c, L_clean, rec, seed=2, scale=0.11, reverse=True, new=True, ws=256)
+        check(H_q, H_k, d, A, L_c, L_clean, rec, seed=2, scale=0.11, reverse=True, new=True, ws=256, dtype=dtype)
     else:
-        check(H_q, H_k, d, A, L_c, L_clean, rec, seed=1, grow=form == "grow")
+        check(H_q, H_k, d, A, L_c, L_clean, rec, seed=1, grow=form == "grow", dtype=dtype)
 
 
 @pytest.mark.parametrize("idx,n,rec", [([0, 1, 2], 0, []), ([2, -1, -1], 1, [2]), ([1, 2, 10 ** 9], 2, [1, 2]), ([0, 1, 2], 77, [0, 1, 2]), ([0, 1, 2], -3, [])])
 @pytest.mark.parametrize("L_c", [20, 300])
-def test_lists(idx, n, rec, L_c):
-    check(4, 2, 64, 3, L_c, 100, rec, idx=idx, n=n)
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32])
+def test_lists(idx, n, rec, L_c, dtype):
+    check(4, 2, 64, 3, L_c, 100, rec, idx=idx, n=n, dtype=dtype)
 
 
 def test_an_entry_that_is_no_chunk_is_skipped():
@@ -153,11 +172,12 @@ def test_equals_the_bf16_attention_of_the_unpacked_rows(H_q, H_k, d, A, L_c, L_c
         assert float((a["lse"] - b["lse"]).abs().max()) < 2.0 ** -7
 
 
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32])
 @pytest.mark.parametrize("L_c", [1, 300])
-def test_a_block_that_is_no_number_shows_only_where_it_is_seen(L_c):
+def test_a_block_that_is_no_number_shows_only_where_it_is_seen(L_c, dtype):
     """A NaN beyond the clean region's end (make() puts one in every spare row) and in slots of later chunks changes nothing."""
     H, d, A, L_clean = 2, 128, 2, 100
-    q, bufs, cap4, slots = make(H, H, d, A, L_c, L_clean, 7)
+    q, bufs, cap4, slots = make(H, H, d, A, L_c, L_clean, 7, dtype=dtype)
     off = [0, L_c]
     args = (L_c, L_clean, off, i32(0, -1), i32(1))
     want = B.flowcache_attend_kv4(q, None, None, *bufs, cap4, *slots, *args)["out"][:L_c].clone()
@@ -167,10 +187,11 @@ def test_a_block_that_is_no_number_shows_only_where_it_is_seen(L_c):
     assert bool(torch.isfinite(want).all()) and torch.equal(got, want)
 
 
-def test_long_buffers():
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32])
+def test_long_buffers(dtype):
     """Codes past 2^32 bytes: a buffer of 2^27 rows, of which the call sees the first, for head 1."""
     H, d, cap4, L_clean, L_c = 2, 64, 1 << 27, 3000, 2
-    q, bufs, small, slots = make(H, H, d, 1, L_c, L_clean, 8)
+    q, bufs, small, slots = make(H, H, d, 1, L_c, L_clean, 8, dtype=dtype)
     big = []
     for b in bufs:
         x = torch.empty(H * cap4 * (d // 2 + d // 32), dtype=torch.uint8, device=DEV)
@@ -182,6 +203,21 @@ def test_long_buffers():
     a = B.flowcache_attend_kv4(q, None, None, *bufs, small, *args)["out"]
     b = B.flowcache_attend_kv4(q, None, None, *big, cap4, *args)["out"]
     assert torch.equal(a, b)
+
+
+@pytest.mark.parametrize("H_q,H_k,d,A,L_c,L_clean", [(12, 12, 128, 2, 300, 2050), (8, 2, 64, 2, 40, 700), (2, 2, 128, 1, 1, 9000)])
+def test_fp32_agrees_with_the_fp32_attention_of_the_unpacked_rows(H_q, H_k, d, A, L_c, L_clean):
+    """Two roundings of the same sums, each within 1e-5 of the norm."""
+    q, bufs, cap4, slots = make(H_q, H_k, d, A, L_c, L_clean, 3, dtype=torch.float32)
+    caches = [torch.zeros((H_k, L_clean + A * L_c, d), device=DEV) for _ in range(2)]
+    B.flowcache_kv4_unpack(*bufs, cap4, *caches, L_clean)
+    for c, s in zip(caches, slots):
+        c[:, L_clean:] = s[:, :A * L_c]
+    off, idx, n = [i * L_c for i in range(A)], i32(*range(A)), i32(A)
+    a = B.flowcache_attend_kv4(q, None, None, *bufs, cap4, *slots, L_c, L_clean, off, idx, n)
+    b = B.flowcache_attend(q, None, None, *caches, L_c, L_clean, [L_clean + o for o in off], idx, n)
+    assert float((a["out"] - b["out"]).norm() / b["out"].norm()) <= 2e-6
+    assert float((a["lse"] - b["lse"]).abs().max()) <= 1e-5
 
 
 def test_another_stream():
@@ -197,7 +233,7 @@ def test_refusals():
         with pytest.raises(ValueError):
             B.flowcache_attend_kv4(**args(**kw))
     for kw in (dict(L_clean=cap4 + 1), dict(active_off=[17]), dict(softmax_scale=-1.0), dict(k4=None, v4=None),
-               dict(q=q.float(), k_cache=slots[0].float(), v_cache=slots[1].float())):
+               dict(L_clean=-1)):
         with pytest.raises(B.FlowCacheError):
             B.flowcache_attend_kv4(**args(**kw))
     for kw in (dict(q=q.float()), dict(k4=None), dict(L_c=4)):
@@ -220,16 +256,18 @@ def sweep(n, seed):
 
 
 @pytest.mark.parametrize("i,shape,grow", sweep(48, 7))
-def test_sweep(i, shape, grow):
-    check(*shape, seed=i, grow=grow, reverse=bool(i & 1), new=bool(i & 2), ws=256 if i % 3 == 0 else None)
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32])
+def test_sweep(i, shape, grow, dtype):
+    check(*shape, seed=i, grow=grow, reverse=bool(i & 1), new=bool(i & 2), ws=256 if i % 3 == 0 else None, dtype=dtype)
 
 
 @pytest.mark.parametrize("L_c,L_clean", [(1, 70), (40, 0), (300, 200), (520, 650)])
-def test_strided_slots(L_c, L_clean):
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32])
+def test_strided_slots(L_c, L_clean, dtype):
     """Slots whose rows are parts of wider ones, heads with a gap: the result of contiguous ones."""
     H, d, A = 3, 128, 2
-    q, bufs, cap4, slots = make(H, H, d, A, L_c, L_clean, 4)
-    wide = [torch.full((H, s.shape[1] + 5, d + 24), float("nan"), device=DEV, dtype=torch.bfloat16)[:, :s.shape[1], 8:8 + d] for s in slots]
+    q, bufs, cap4, slots = make(H, H, d, A, L_c, L_clean, 4, dtype=dtype)
+    wide = [torch.full((H, s.shape[1] + 5, d + 24), float("nan"), device=DEV, dtype=dtype)[:, :s.shape[1], 8:8 + d] for s in slots]
     for w, s in zip(wide, slots):
         w.copy_(s)
     args = (L_c, L_clean, [L_c + 2, 0], i32(0, 1), i32(2))

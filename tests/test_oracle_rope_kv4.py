@@ -188,7 +188,7 @@ def test_attend_kv4_rejects_bad_arguments(L):
 
     for name in ("q", "k_new", "v_new", "k4", "v4", "kc", "vc", "off", "idx", "n", "out"):
         assert attend(**{name: NULL}) == INVALID, name
-    assert attend(dtype=0) == UNSUPPORTED and attend(dtype=5) == INVALID
+    assert attend(dtype=5) == INVALID and attend(dtype=0, ts=66, hs=256 * 66) == UNSUPPORTED
     assert attend(cap4=511) == INVALID and attend(L_clean=-1) == INVALID
     assert attend(H_q=3, H_k=2) == INVALID and attend(A=0) == INVALID and attend(A=17) == INVALID and attend(L_c=0) == INVALID
     assert attend(d=96) == UNSUPPORTED and attend(ts=32) == INVALID and attend(hs=100) == INVALID
