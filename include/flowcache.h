@@ -390,7 +390,7 @@ size_t flowcache_kv_compress_status_offset(int H_k, int L_k, int d, int budget, 
  * (but for q_out = q).
  * Errors: null pointers, grid_h or grid_w < 1, theta < 1 or not finite, norm_eps < 0 or not finite,
  * dims odd, negative or beyond d, slots outside the cache or overlapping -> FC_INVALID_ARGUMENT; d not in
- * {64, 128}, strides or pointers that are not multiples of 16 bytes -> FC_UNSUPPORTED.
+ * {64, 128}, strides or pointers that are not multiples of 16 bytes, L_c above 2^27 - 8 -> FC_UNSUPPORTED.
  */
 typedef enum { FC_ROPE_INTERLEAVED = 0, FC_ROPE_HALVES = 1 } fc_rope_pairing;
 int flowcache_qk_norm_rope(const void* q, int64_t q_tok_stride, const void* k, const void* v,
@@ -427,8 +427,8 @@ int flowcache_qk_norm_rope(const void* q, int64_t q_tok_stride, const void* k, c
  *                  stays as it was
  *   k_cache, v_cache, strides, capacity    as in flowcache_attend
  * count = 0 does nothing.  Errors: rows outside [0, capacity) or [0, capacity4), null pointers ->
- * FC_INVALID_ARGUMENT; d not in {64, 128}, misaligned pointers or strides -> FC_UNSUPPORTED.
- * flowcache_kv4_bytes gives 0 for invalid arguments.
+ * FC_INVALID_ARGUMENT; d not in {64, 128}, misaligned pointers or strides, more than 2^27 - 8 rows ->
+ * FC_UNSUPPORTED.  flowcache_kv4_bytes gives 0 for invalid arguments.
  */
 size_t flowcache_kv4_bytes(int H_k, int capacity4, int d);
 int flowcache_kv4_pack(const void* k_cache, const void* v_cache, int64_t kv_head_stride,
@@ -450,7 +450,7 @@ int flowcache_kv4_unpack(const void* k4, const void* v4, int capacity4, int pos4
  *   dtype    type of q, the caches and out.  The 4-bit values are operands without rounding, so the result
  *            is flowcache_attend's on the unpacked rows.  fp32 elements of q (times the scale) and of the
  *            slots keep all their bits if they are 0 or from 2^-100 to 2^127 in magnitude
- * More than 2^31 - 257 visible positions -> FC_UNSUPPORTED.
+ * More than 2^31 - 257 visible positions or A * H_q * ceil(L_c / 32) of 2^23 - 8 and more -> FC_UNSUPPORTED.
  * The importance mass is not emitted here: at a commit the clean keys are unpacked for the selection
  * anyway, and flowcache_attention_mass takes them from there.
  */

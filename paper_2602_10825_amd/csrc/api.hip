@@ -265,6 +265,9 @@ int flowcache_attend(const void* q, const void* k_new, const void* v_new, void* 
     return FC_OK;
 }
 
+// Rows of a launch whose blocks of 256 threads take 8 of them or more: a dimension of a grid is below 2^32 threads.
+static constexpr int kMostRows = (1 << 27) - 8;
+
 // ------------------------------------------------------------------ qk_norm_rope
 int flowcache_qk_norm_rope(const void* q, int64_t q_tok_stride, const void* k, const void* v,
                            int64_t kv_new_tok_stride, fc_dtype dtype, int H_q, int H_k, int d,
@@ -296,7 +299,7 @@ int flowcache_qk_norm_rope(const void* q, int64_t q_tok_stride, const void* k, c
     if (q_tok_stride < (int64_t)H_q * d || kv_new_tok_stride < (int64_t)H_k * d) return FC_INVALID_ARGUMENT;
     if (q_tok_stride % per16 != 0 || kv_new_tok_stride % per16 != 0) return FC_UNSUPPORTED;
     if (!aligned16(q) || !aligned16(k) || !aligned16(v) || !aligned16(q_out)) return FC_UNSUPPORTED;
-    if ((int64_t)A * L_c > INT32_MAX || (int64_t)grid_h * grid_w > INT32_MAX) return FC_UNSUPPORTED;
+    if (L_c > kMostRows || (int64_t)A * L_c > INT32_MAX || (int64_t)grid_h * grid_w > INT32_MAX) return FC_UNSUPPORTED;
 
     FcRopeArgs a{};
     a.q = q; a.k = k; a.v = v; a.q_stride = q_tok_stride; a.kv_stride = kv_new_tok_stride;
@@ -335,7 +338,7 @@ int check_kv4(const FcKv4Args& a, int capacity) {
     const int st = check_kv_layout(a.k_cache, a.v_cache ? a.v_cache : a.k_cache, a.head_stride, a.tok_stride, capacity, a.dtype, a.H_k, a.d);
     if (st != FC_OK) return st;
     // (heads are a dimension of the launch's grid)
-    return aligned16(a.k4) && aligned16(a.v4) && a.H_k <= 65535 ? FC_OK : FC_UNSUPPORTED;
+    return aligned16(a.k4) && aligned16(a.v4) && a.H_k <= 65535 && a.count <= kMostRows ? FC_OK : FC_UNSUPPORTED;
 }
 }  // namespace
 
@@ -382,9 +385,11 @@ int flowcache_attend_kv4(const void* q, const void* k_new, const void* v_new, co
     if (st != FC_OK) return st;
     if (H_q % H_k != 0) return FC_INVALID_ARGUMENT;
     if (!(softmax_scale >= 0.f) || !std::isfinite(softmax_scale)) return FC_INVALID_ARGUMENT;
-    if ((int64_t)L_clean + (int64_t)A * L_c > INT32_MAX - 256) return FC_UNSUPPORTED;   // (kernels round up to tiles)
     st = check_slots(A, L_c, 0, capacity, active_off);
     if (st != FC_OK) return st;
+    if ((int64_t)L_clean + (int64_t)A * L_c > INT32_MAX - 256) return FC_UNSUPPORTED;   // (kernels round up to tiles)
+    // (blocks of 32 rows and 512 threads, below 2^32 threads)
+    if ((int64_t)A * H_q * (((int64_t)L_c + 31) / 32) >= (1 << 23) - 8) return FC_UNSUPPORTED;
     if (!aligned16(q) || !aligned16(out) || (k_new && (!aligned16(k_new) || !aligned16(v_new))) ||
         (L_clean > 0 && (!aligned16(k4) || !aligned16(v4))))
         return FC_UNSUPPORTED;

@@ -148,7 +148,6 @@ int launch(const FcRopeArgs& a, hipStream_t s) {
     int64_t slices = (2048 + groups - 1) / groups;
     slices = slices < total ? slices : total;
     const int64_t blocks = (groups * slices + kWaves - 1) / kWaves;
-    if (blocks > INT32_MAX / kWaves) return FC_UNSUPPORTED;
     if (a.pairing)
         qk_norm_rope_kernel<T, D, true><<<dim3((unsigned)blocks, a.A), kThreads, 0, s>>>(a, (int)slices);
     else

@@ -144,6 +144,7 @@ def test_qk_norm_rope_rejects_bad_arguments(L):
     assert rope(L, hs=100) == INVALID and rope(L, ts=64) == INVALID
     for name in ("q", "k", "v", "out", "kc", "vc"):
         assert rope(L, **{name: ctypes.c_void_p(0x10008)}) == UNSUPPORTED, name
+    assert rope(L, L_c=2 ** 27 - 7, A=1, off=ints(0), frame0=ints(0), cap=2 ** 28, hs=2 ** 28 * 128, L_clean=0) == UNSUPPORTED
     assert rope(L, L_c=2 ** 30, A=2, off=ints(0, 2 ** 30 - 1), cap=2 ** 31 - 1, hs=2 ** 40, L_clean=0) == INVALID
 
 
@@ -173,6 +174,7 @@ def test_kv4_rejects_bad_arguments(L):
         assert call(d=32) == UNSUPPORTED and call(hs=499 * 64) == INVALID and call(ts=63) == INVALID and call(ts=68, hs=500 * 68) == UNSUPPORTED
         assert call(k4=ctypes.c_void_p(0x10004)) == UNSUPPORTED and call(vc=ctypes.c_void_p(0x10002)) == UNSUPPORTED
         assert call(H=65536) == UNSUPPORTED
+        assert call(count=2 ** 27 - 7, cap=2 ** 27, hs=2 ** 33, cap4=2 ** 27) == UNSUPPORTED
         assert call(count=0) == 0                                        # nothing to do, nothing launched
         assert call(count=0, v4=NULL, vc=NULL) == 0                      # K alone
     assert pack(kept=P, pos=1) == INVALID                                # rows from a list start nowhere
@@ -199,5 +201,7 @@ def test_attend_kv4_rejects_bad_arguments(L):
         assert attend(**{name: ctypes.c_void_p(0x10004)}) == UNSUPPORTED, name
     assert attend(L_clean=2 ** 31 - 200, cap4=2 ** 31 - 1) == UNSUPPORTED  # positions beyond 32 bits
     assert attend(L_clean=2 ** 31 - 256 - 256, cap4=2 ** 31 - 1) == UNSUPPORTED     # or so near that a tile passes them
+    for dtype in (0, 1):                                 # a launch of 2^32 threads
+        assert attend(dtype=dtype, L_c=2 ** 24, off=ints(0, 2 ** 24), cap=2 ** 25, hs=2 ** 31, H_q=16) == UNSUPPORTED
     assert L.flowcache_attend_kv4_workspace(2, 128, 4, 64) == L.flowcache_attend_workspace(2, 128, 4, 1, 64, 0, 50)
     assert L.flowcache_attend_kv4_workspace(0, 128, 4, 64) == 0 and L.flowcache_attend_kv4_workspace(2, 128, 4, 96) == 0
