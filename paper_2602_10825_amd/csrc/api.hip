@@ -411,11 +411,7 @@ int flowcache_attend_kv4(const void* q, const void* k_new, const void* v_new, co
     at.ws = workspace; at.ws_bytes = workspace ? workspace_bytes : 0;
     const int64_t rows = L_clean > 0 ? capacity4 : 0;
     const FcKv4 clean4{(const uint8_t*)k4, (const uint8_t*)v4, rows * (d / 2), rows * (d / 32), H_k * rows * (d / 2), L_clean};
-    const hipStream_t s = (hipStream_t)stream;
-    if (dtype == FC_BF16) return fc_launch_attend_kv4(at, clean4, s);
-    // fp32 without clean rows: 256-row blocks, which split a slot's rows once for all of them (24 x 128, 4 x 2340 rows 3.4 ms
-    // against 5.1 in 32-row blocks)
-    return L_clean == 0 ? fc_launch_attend_f32(at, s) : fc_launch_attend_kv4_f32(at, clean4, s);
+    return dtype == FC_BF16 ? fc_launch_attend_kv4(at, clean4, (hipStream_t)stream) : fc_launch_attend_kv4_f32(at, clean4, (hipStream_t)stream);
 }
 
 // ------------------------------------------------------------------ kv_compress

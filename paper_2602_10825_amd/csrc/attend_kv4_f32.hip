@@ -1,19 +1,17 @@
 // Chunk-causal attention of fp32 queries on a clean region in 4 bits (kv4.hpp) and the active chunks' fp32 slots.  Products on
 // the bf16 matrix cores, floats in three bf16 parts (f32_split.hpp).  A value of the 4-bit rows has two significant
 // bits and is its own first part, so a product with it takes three of the six: a clean key costs half of
-// what it costs attend_f32.hip's blocks, which also read 16 times its bytes.
-//
-// 32 query rows per block; its 8 wavefronts take every 8th 32-key tile of the range, as in attend_kv4.hip (FcAttendArgs
-// describes the slots alone, the clean region's tiles come first).  Q's parts are in LDS for all wavefronts.  K's codes go straight
-// into the product's operand, V's become bf16 rows in LDS that a transposing read turns; a slot's V is taken 32 columns at a time,
-// its parts side by side in the same LDS.
-// 12 x 128, on codes and the chunk's own slot: 256 rows on 49201 keys 220 us (attend_f32.hip on the unpacked rows 372), 353 TFLOP/s
-// where a third of a large bf16 product's rate is 394: the matrix cores; one row on 61201 keys 47 us (200); 10200 rows on 40800
-// keys and two slots 15.8 ms (16.8).  There the slots take half of the time, bound by the vector instructions that split their
-// rows, 700 of 900 per tile: 130 TFLOP/s (attend_f32.hip's 256-row blocks: 197).
+// what it costs attend_f32.hip, which also reads 16 times its bytes.  Bodies, plan and divisions of the keys as there.
+// us, attend_f32.hip on the unpacked rows / here: 12 x 128, one row on 61201 keys 200 / 47, 256 rows on 49201 372 / 211, 600 on 5200
+// 134 / 78, 10200 on 40800 keys and two slots 16600 / 11830; 24 x 128, 2 chunks of 4000 rows on 20000 keys 10870 / 7440, 4 of 2340 on
+// their slots alone 3360 / 3240; 24 x 64, 2 of 2040 rows on 18360 keys and 5 slots 3040 / 2440.
+// The large ones run at 325 .. 380 TFLOP/s counted as fp32, where a third (codes) and a sixth (slots) of a large bf16 product's rate are
+// 394 and 197: matrix cores.
 //
 // Operands are finite; a part is lost below 2^-110, so entries of Q (times the scale) and of the slots hold all their bits from
 // 2^-100 on.
+#include <type_traits>
+
 #include "attend_split.hpp"
 #include "f32_split.hpp"
 #include "kv4_tiles.hpp"
@@ -25,8 +23,15 @@ constexpr int NT = kSplitThreads;
 // The exponents' reference is raised this far beyond the row maximum when that passes it (log2): weights are at most 1.
 constexpr float kAhead = 4.0f;
 
+// ---- few query rows ---------------------------------------------------------------------
+// 32 query rows per block; its 8 wavefronts take every 8th 32-key tile of the range, as in attend_kv4.hip (FcAttendArgs
+// describes the slots alone, the clean region's tiles come first).  Q's parts are in LDS for all wavefronts.  K's codes go straight
+// into the product's operand, V's become bf16 rows in LDS that a transposing read turns; a slot's V is taken 32 columns at a time,
+// its parts side by side in the same LDS.  On codes 353 TFLOP/s of those 394; a slot's tile takes three times as long, 40 % of it waiting
+// for its rows, which are too many to have two on their way.  Tried there: rows read in whole lines (the same), residues of
+// the splitting by products of pairs instead of shifts (a third fewer vector instructions, the same).
 template <int D>
-struct Smem {
+struct NarrowSmem {
     static constexpr int QROW = D + 8, OROW = D + 4;
     static constexpr int TILE = 32 * (D > 3 * 32 ? D : 3 * 32);      // a tile of codes, or 32 columns of a slot's in three parts
     __attribute__((aligned(16))) union {
@@ -41,15 +46,13 @@ struct Smem {
 };
 
 template <int D>
-__global__ __launch_bounds__(NT) void attend_kv4_f32_kernel(FcAttendArgs a, FcAttendPlan p, float* parts, FcKv4 x) {
+__device__ __forceinline__ void attend_narrow(const FcAttendArgs& a, const FcAttendPlan& p, uint32_t valid, NarrowSmem<D>& sm,
+                                              float* parts, const FcKv4& x) {
     constexpr int KS = D / 16;           // contraction steps of Q K^T
     constexpr int NB = D / 32;           // 32-wide blocks of the value dimension
-    constexpr int QROW = Smem<D>::QROW, OROW = Smem<D>::OROW;
-    __shared__ Smem<D> sm;
+    constexpr int QROW = NarrowSmem<D>::QROW, OROW = NarrowSmem<D>::OROW;
     Segments& sg = sm.sg;
 
-    const uint32_t valid = valid_blocks(a);
-    if (valid == 0u) return;
     const SplitItem it = split_item(a, p, valid, blockIdx.x);
     if (!it.ok) return;
     const int hk = it.h / (a.H_q / a.H_k);
@@ -275,19 +278,347 @@ __global__ __launch_bounds__(NT) void attend_kv4_f32_kernel(FcAttendArgs a, FcAt
     finish_unit<float, D, OROW>(a, p, it, sm.o, sm.m_s, sm.l_s, parts);
 }
 
-// 32-row blocks for every recompute count; how many ranges the keys of a block are divided into.
-FcAttendPlan plan_of(const FcAttendArgs& a, int L_clean, bool may_split) {
-    FcAttendPlan p{};
-    p.tiles = (a.L_c + kUnitRows - 1) / kUnitRows;
-    const int64_t keys = (int64_t)L_clean + (int64_t)a.A * a.L_c;
-    for (int R = 1; R <= a.A; ++R) {
-        int S = 1;
-        const int64_t units = (int64_t)R * a.H_q * p.tiles;
-        fc_narrow_cost(units, (int)((keys + BK - 1) / BK), 14, may_split, &S);
-        p.narrow[R - 1] = 1;
-        fc_plan_add(p, R, units * S, units, S);
+// ---- many query rows ----------------------------------------------------------------------------
+// The 256-row body of attend_f32.hip: Q in registers, every 32-key tile read once, turned into parts once and double-buffered in
+// LDS, a tile's contribution to O summed up by itself (added up in O directly: 11280 instead of 11830 us on 12 x 128, 10200 rows
+// on 40800 keys, but a relative error of 24e-7 instead of 9e-7, which is attend_f32.hip's).  A tile of codes has one part
+// and three products.  There is a loop for tiles of codes and one for slots' (at every step's choice between them the registers of both
+// would be live), and one step that goes from the one to the other.
+template <int D>
+struct WideSmem {
+    static constexpr int KROW = D + 8, VROW = D + 32;
+    __attribute__((aligned(16))) bf16_t K[2][3][BK * KROW], V[2][3][BK * VROW];   // [buffer][part]; of codes the first part alone
+    static constexpr int QL = D == 128 ? 6 : 0;      // steps of which Q's last part is kept here, every wavefront's own
+    u32x4_native ql[QL > 0 ? QL : 1][kSplitWaves][FC_WAVE];
+    Segments sg;
+};
+
+template <int D>
+__device__ __forceinline__ void attend_wide(const FcAttendArgs& a, const FcAttendPlan& p, uint32_t valid, WideSmem<D>& sm,
+                                            float* parts, const FcKv4& x4) {
+    constexpr int KS = D / 16;           // contraction steps of Q K^T
+    constexpr int NB = D / 32;           // 32-wide blocks of the value dimension
+    constexpr int KROW = WideSmem<D>::KROW, VROW = WideSmem<D>::VROW, QL = WideSmem<D>::QL;
+    constexpr int EPT = BK * D / NT;     // entries of K, and of V, per thread and tile: all of one row
+    constexpr int LPR = D / EPT;         // threads per row
+    typedef uint32_t word_t __attribute__((ext_vector_type(EPT / 2)));
+    static_assert(EPT == 8 || EPT == 4, "a thread's codes are 4 bytes or 2");
+    typedef std::conditional_t<EPT == 8, uint32_t, uint16_t> codes_t;
+    Segments& sg = sm.sg;
+
+    const WideItem wi = wide_item<true>(a, p, valid, blockIdx.x);
+    if (!wi.ok) return;
+    const int hk = wi.h / (a.H_q / a.H_k);
+    const int tid = threadIdx.x;
+    const int wave = __builtin_amdgcn_readfirstlane(tid >> 6), lane = tid & 63;
+    const int l32 = lane & 31, hh = lane >> 5, l16 = lane & 15;
+    const float c2 = a.scale * 1.4426950408889634f;
+    if (tid == 0) list_segments(a, a.rec_idx[wi.r], sg);
+
+    // B operand of S^T = K Q^T: lane holds Q[q = l32][16 st + 8 hh .. + 8)
+    const int row_in_chunk = wi.tile * kWideRows + wave * 32 + l32;
+    const float* q_row = (const float*)a.q + (((int64_t)wi.r * a.L_c + (row_in_chunk > a.L_c - 1 ? a.L_c - 1 : row_in_chunk)) * a.H_q + wi.h) * D;
+    Split8 qf[KS];
+#pragma unroll
+    for (int st = 0; st < KS; ++st) {
+        const f32x4_t x0 = *reinterpret_cast<const f32x4_t*>(q_row + 16 * st + 8 * hh) * c2;
+        const f32x4_t x1 = *reinterpret_cast<const f32x4_t*>(q_row + 16 * st + 8 * hh + 4) * c2;
+        split_pair(qf[st], 0, x0[0], x0[1]); split_pair(qf[st], 1, x0[2], x0[3]);
+        split_pair(qf[st], 2, x1[0], x1[1]); split_pair(qf[st], 3, x1[2], x1[3]);
+        if (st < QL) sm.ql[st][wave][lane] = qf[st].l;
     }
-    return p;
+    __syncthreads();
+
+    const int tiles4 = (x4.L_clean + BK - 1) / BK;
+    const int nt_all = tiles4 + __builtin_amdgcn_readfirstlane(sg.tile0[sg.n]);
+    const int t_lo = (int)((int64_t)nt_all * wi.s / wi.S), nt = (int)((int64_t)nt_all * (wi.s + 1) / wi.S) - t_lo;
+    const int n_codes = tiles4 - t_lo < 0 ? 0 : tiles4 - t_lo < nt ? tiles4 - t_lo : nt;    // the range's first tiles
+
+    f32x16_t o[NB];
+#pragma unroll
+    for (int b = 0; b < NB; ++b)
+#pragma unroll
+        for (int i = 0; i < 16; ++i) o[b][i] = 0.f;
+    float m = kNegBig, l = 0.f;
+
+    // tile t of the range -> registers, entries of one row per thread; rows past the end: the last one again
+    const int ld_row = tid / LPR, ld_col = EPT * (tid % LPR);
+    int nv_load = BK;                                 // valid keys of the tile loaded last
+    uint32_t kc = 0, vc = 0, ks = 0, vs = 0;
+    auto load_codes = [&](int t) __attribute__((always_inline)) {
+        const int tt = t_lo + t, left = x4.L_clean - tt * BK;
+        nv_load = left < BK ? left : BK;
+        const uint32_t row = (uint32_t)(ld_row < nv_load ? ld_row : nv_load - 1);
+        const int64_t codes = (int64_t)hk * x4.head_codes + (int64_t)tt * (BK * D / 2), scales = x4.scales_at + (int64_t)hk * x4.head_scales + (int64_t)tt * D;
+        const uint32_t at = row * (D / 2) + ld_col / 2, s_at = row * (D / 32) + ld_col / 32;
+        kc = *reinterpret_cast<const codes_t*>(x4.k + codes + at);
+        vc = *reinterpret_cast<const codes_t*>(x4.v + codes + at);
+        ks = *(x4.k + scales + s_at);
+        vs = *(x4.v + scales + s_at);
+    };
+    f32x4_t kr[EPT / 4], vr[EPT / 4];
+    const float* kbase = (const float*)a.k_cache + (int64_t)hk * a.head_stride;
+    const float* vbase = (const float*)a.v_cache + (int64_t)hk * a.head_stride;
+    const uint32_t ts = (uint32_t)a.tok_stride;
+    int seg = 0;
+    auto load_rows = [&](int t) __attribute__((always_inline)) {
+        const int tt = t_lo + t - tiles4;
+        while (tt >= __builtin_amdgcn_readfirstlane(sg.tile0[seg + 1])) ++seg;
+        const int off = (tt - __builtin_amdgcn_readfirstlane(sg.tile0[seg])) * BK;
+        const int left = __builtin_amdgcn_readfirstlane(sg.len[seg]) - off;
+        const int64_t pos = (int64_t)(__builtin_amdgcn_readfirstlane(sg.start[seg]) + off) * a.tok_stride;
+        nv_load = left < BK ? left : BK;
+        const uint32_t at = (uint32_t)(ld_row < nv_load ? ld_row : nv_load - 1) * ts + (uint32_t)ld_col;
+#pragma unroll
+        for (int j = 0; j < EPT / 4; ++j) {
+            kr[j] = *reinterpret_cast<const f32x4_t*>(kbase + pos + at + 4 * j);
+            vr[j] = *reinterpret_cast<const f32x4_t*>(vbase + pos + at + 4 * j);
+        }
+    };
+    // What lies beyond the 16 bits of an access's own offset is reached from addresses that the compiler takes as given (or it
+    // keeps one register for each access).
+    auto given = [&](auto* at) __attribute__((always_inline)) {
+        uint32_t off = (uint32_t)(reinterpret_cast<char*>(at) - reinterpret_cast<char*>(&sm));
+        asm("" : "+v"(off));
+        return reinterpret_cast<decltype(at)>(reinterpret_cast<char*>(&sm) + off);
+    };
+    bf16_t* const v_st = given(&sm.V[0][0][ld_row * VROW + ld_col]);
+    const u32x4_native* const ql_at = given(&sm.ql[0][wave][lane]);
+    const int st_k = ld_row * KROW + ld_col;
+    auto store_part = [&](bf16_t* at, const u32x4_native& x) __attribute__((always_inline)) {
+        word_t w;
+#pragma unroll
+        for (int i = 0; i < EPT / 2; ++i) w[i] = x[i];
+        *reinterpret_cast<word_t*>(at) = w;
+    };
+    // The loaded tile into buffer `buf`, in KS pieces: codes in the first two, of rows a pair of K's or V's entries each.
+    Split8 sp;
+    auto stage = [&](auto codes, int buf, int e) __attribute__((always_inline)) {
+        if constexpr (decltype(codes)::value) {
+            if (e == 0) store_part(&sm.K[buf][0][st_k], fc_kv4_to_bf16(kc, ks));
+            if (e == 1) store_part(v_st + buf * (3 * BK * VROW), fc_kv4_to_bf16(vc, vs));
+        } else {
+            const bool v = e >= EPT / 2;
+            const int i = v ? e - EPT / 2 : e;
+            const f32x4_t& f = v ? vr[i >> 1] : kr[i >> 1];
+            split_pair(sp, i, f[2 * (i & 1)], f[2 * (i & 1) + 1]);
+            if (i < EPT / 2 - 1) return;
+#pragma unroll
+            for (int part = 0; part < 3; ++part)
+                store_part(v ? v_st + (buf * 3 + part) * (BK * VROW) : &sm.K[buf][part][st_k], part == 0 ? sp.h : part == 1 ? sp.m : sp.l);
+        }
+    };
+    const int k_frag = l32 * KROW + 8 * hh;
+    const bf16_t* const v_at = given(&sm.V[0][0][(hh * 4 + (l16 >> 2)) * VROW + ((lane >> 4) & 1) * 16 + (l16 & 3) * 4]);
+    auto read_k = [&](int buf, int part, int st) __attribute__((always_inline)) {
+        return *reinterpret_cast<const u32x4_native*>(&sm.K[buf][part][k_frag + 16 * st]);
+    };
+    auto read_v = [&](int buf, int part, int g) __attribute__((always_inline)) {    // g: value block g / 2, 16-key step g % 2
+        const bf16_t* vp = v_at + ((buf * 3 + part) * (BK * VROW) + (g % 2) * 16 * VROW + (g / 2) * 32);
+        const s16x4_t lo = lds_read_tr(vp), hi = lds_read_tr(vp + 8 * VROW);
+        return __builtin_bit_cast(u32x4_native, __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7));
+    };
+
+    int nv = 0;
+    // Tile t, which is one of codes or not, as tile t + 1 is
+    auto step = [&](auto codes, auto next_codes, int t) __attribute__((always_inline)) {
+        constexpr bool C = decltype(codes)::value;
+        const int buf = t & 1;
+        f32x16_t s;
+#pragma unroll
+        for (int i = 0; i < 16; ++i) s[i] = 0.f;
+        auto q_last = [&](int st) __attribute__((always_inline)) { return st < QL ? ql_at[st * (kSplitWaves * FC_WAVE)] : qf[st].l; };
+        // the smaller products first: then only the largest ones, K's first parts read once more, round the scores' bits
+        __builtin_amdgcn_s_setprio(1);
+        if constexpr (C) {
+            u32x4_native f0 = read_k(buf, 0, 0), f1;
+#pragma unroll
+            for (int st = 0; st < KS; ++st) {
+                f1 = read_k(buf, 0, (st + 1) % KS);
+                const u32x4_native ql = q_last(st);
+                split_mfma(f0, ql, s);
+                __builtin_amdgcn_sched_barrier(0);
+                stage(next_codes, buf ^ 1, st);
+                split_mfma(f0, qf[st].m, s);
+                __builtin_amdgcn_sched_barrier(0);
+                f0 = f1;
+            }
+#pragma unroll
+            for (int st = 0; st < KS; ++st) {
+                if (st + 1 < KS) f1 = read_k(buf, 0, st + 1);
+                split_mfma(f0, qf[st].h, s);
+                __builtin_amdgcn_sched_barrier(0);
+                f0 = f1;
+            }
+        } else {
+            Split8 f0 = {read_k(buf, 0, 0), read_k(buf, 1, 0), read_k(buf, 2, 0)}, f1;
+            u32x4_native h0, h1, h2;
+#pragma unroll
+            for (int st = 0; st < KS; ++st) {
+                if (st + 1 < KS) f1 = Split8{read_k(buf, 0, st + 1), read_k(buf, 1, st + 1), read_k(buf, 2, st + 1)};
+                else { h0 = read_k(buf, 0, 0); h1 = read_k(buf, 0, 1); }
+                const u32x4_native ql = q_last(st);
+                split_mfma(f0.l, qf[st].h, s);
+                split_mfma(f0.m, qf[st].m, s);
+                __builtin_amdgcn_sched_barrier(0);
+                stage(next_codes, buf ^ 1, st);
+                split_mfma(f0.m, qf[st].h, s);
+                split_mfma(f0.h, ql, s);
+                split_mfma(f0.h, qf[st].m, s);
+                __builtin_amdgcn_sched_barrier(0);
+                f0 = f1;
+            }
+#pragma unroll
+            for (int st = 0; st < KS; ++st) {
+                if (st + 2 < KS) h2 = read_k(buf, 0, st + 2);
+                split_mfma(h0, qf[st].h, s);
+                __builtin_amdgcn_sched_barrier(0);
+                h0 = h1;
+                h1 = h2;
+            }
+        }
+        __builtin_amdgcn_s_setprio(0);
+        auto read_parts = [&](int g) __attribute__((always_inline)) {
+            if constexpr (C) return read_v(buf, 0, g);
+            else return Split8{read_v(buf, 0, g), read_v(buf, 1, g), read_v(buf, 2, g)};
+        };
+        auto va = read_parts(0), na = va;
+        if (nv < BK) {
+            const int mine = nv - hh * 4;
+#pragma unroll
+            for (int i = 0; i < 16; ++i)
+                if ((i >> 2) * 8 + (i & 3) >= mine) s[i] = kNegBig;
+        }
+        nv = nv_load;                                  // of tile t + 1
+        float mx = s[0];
+#pragma unroll
+        for (int i = 1; i < 16; ++i) mx = fmaxf(mx, s[i]);
+        if (__any(mx > m)) {
+            const float top = fmaxf(mx, __shfl_xor(mx, 32, FC_WAVE)), mn = top > m ? top + kAhead : m;
+            const float alpha = __builtin_amdgcn_exp2f(m - mn);
+            m = mn;
+            l *= alpha;
+#pragma unroll
+            for (int b = 0; b < NB; ++b) o[b] *= alpha;
+        }
+        float p0 = 0.f, p1 = 0.f;
+        Split8 ps[2];
+        auto weights = [&](int i) __attribute__((always_inline)) {      // of accumulators i and i + 1
+            const float x0 = __builtin_amdgcn_exp2f(s[i] - m), x1 = __builtin_amdgcn_exp2f(s[i + 1] - m);
+            p0 += x0;
+            p1 += x1;
+            split_pair(ps[i >> 3], (i & 7) >> 1, x0, x1);
+        };
+#pragma unroll
+        for (int i = 0; i < 8; i += 2) weights(i);
+        f32x16_t x;
+#pragma unroll
+        for (int g = 0; g < 2 * NB; ++g) {                 // value block g / 2, 16-key step g % 2
+            if (g % 2 == 0) {
+#pragma unroll
+                for (int i = 0; i < 16; ++i) x[i] = 0.f;
+            }
+            if (g + 1 < 2 * NB) na = read_parts(g + 1);
+            const Split8& pc = ps[g % 2];
+            if constexpr (C) {
+                split_mfma(va, pc.l, x); if (g == 0) { weights(8); weights(10); } __builtin_amdgcn_sched_barrier(0);
+                split_mfma(va, pc.m, x); if (g == 0) { weights(12); weights(14); } __builtin_amdgcn_sched_barrier(0);
+                split_mfma(va, pc.h, x);
+            } else {
+                split_mfma(va.l, pc.h, x); if (g == 0) weights(8); __builtin_amdgcn_sched_barrier(0);
+                split_mfma(va.h, pc.l, x); if (g == 0) weights(10); __builtin_amdgcn_sched_barrier(0);
+                split_mfma(va.m, pc.m, x); if (g == 0) weights(12); __builtin_amdgcn_sched_barrier(0);
+                split_mfma(va.m, pc.h, x); if (g == 0) weights(14); __builtin_amdgcn_sched_barrier(0);
+                split_mfma(va.h, pc.m, x); __builtin_amdgcn_sched_barrier(0);
+                split_mfma(va.h, pc.h, x);
+            }
+            va = na;
+            if (g % 2 == 1) o[g / 2] += x;
+            if (g == 1 && t + 2 < nt) {                    // (the scores' registers are free)
+                if (decltype(next_codes)::value && t + 2 < n_codes) load_codes(t + 2);
+                else load_rows(t + 2);
+            }
+        }
+        l += p0 + p1;
+        lds_barrier();
+    };
+    if (nt > 0) {
+        const std::true_type codes;
+        const std::false_type rows;
+        if (n_codes > 0) {
+            load_codes(0);
+            nv = nv_load;
+#pragma unroll
+            for (int e = 0; e < KS; ++e) stage(codes, 0, e);
+        } else {
+            load_rows(0);
+            nv = nv_load;
+#pragma unroll
+            for (int e = 0; e < KS; ++e) stage(rows, 0, e);
+        }
+        if (nt > 1) {
+            if (n_codes > 1) load_codes(1);
+            else load_rows(1);
+        }
+        lds_barrier();
+        int t = 0;
+        const int whole = n_codes < nt ? n_codes - 1 : nt;         // tiles of codes before another (or nothing)
+#pragma unroll 1
+        for (; t < whole; ++t) step(codes, codes, t);
+        if (t < n_codes) { step(codes, rows, t); ++t; }
+#pragma unroll 1
+        for (; t < nt; ++t) step(rows, rows, t);
+    }
+
+    const float ltot = l + __shfl_xor(l, 32, FC_WAVE);
+    if (wi.S > 1) {
+        const int64_t part = (wi.unit * (kWideRows / kUnitRows) + wave) * wi.S + wi.s;   // 32 rows each
+        float* po = parts + (part * kUnitRows + l32) * D;
+#pragma unroll
+        for (int b = 0; b < NB; ++b)
+#pragma unroll
+            for (int g = 0; g < 4; ++g)
+                store_out(po + b * 32 + g * 8 + hh * 4, o[b][4 * g], o[b][4 * g + 1], o[b][4 * g + 2], o[b][4 * g + 3]);
+        if (hh == 0) {
+            float* ml = parts + (int64_t)p.parts * kUnitRows * D + part * 2 * kUnitRows;
+            ml[l32] = m;
+            ml[kUnitRows + l32] = ltot;
+        }
+        return;
+    }
+    if (row_in_chunk >= a.L_c) return;
+    const float inv = 1.0f / ltot;
+    const int64_t row = (int64_t)wi.r * a.L_c + row_in_chunk;
+    float* op = (float*)a.out + (row * a.H_q + wi.h) * D;
+#pragma unroll
+    for (int b = 0; b < NB; ++b)
+#pragma unroll
+        for (int g = 0; g < 4; ++g)
+            store_out(op + b * 32 + g * 8 + hh * 4, o[b][4 * g] * inv, o[b][4 * g + 1] * inv, o[b][4 * g + 2] * inv, o[b][4 * g + 3] * inv);
+    if (a.lse && hh == 0)
+        a.lse[(int64_t)wi.h * a.A * a.L_c + row] = (m + __builtin_amdgcn_logf(ltot)) * 0.6931471805599453f;
+}
+
+// WIDE and NARROW say which of the two bodies some recompute count of this launch asks for.
+template <int D, bool WIDE, bool NARROW>
+__global__ __launch_bounds__(NT) void attend_kv4_f32_kernel(FcAttendArgs a, FcAttendPlan p, float* parts, FcKv4 x) {
+    const uint32_t valid = valid_blocks(a);
+    const int R = __popc(valid);
+    if (R == 0) return;
+    constexpr size_t w = WIDE ? sizeof(WideSmem<D>) : 0, n = NARROW ? sizeof(NarrowSmem<D>) : 0;
+    __shared__ __attribute__((aligned(16))) char raw[w > n ? w : n];
+    if (WIDE && (!NARROW || !p.narrow[R - 1]))
+        attend_wide<D>(a, p, valid, *reinterpret_cast<WideSmem<D>*>(raw), parts, x);
+    else if (NARROW)
+        attend_narrow<D>(a, p, valid, *reinterpret_cast<NarrowSmem<D>*>(raw), parts, x);
+}
+
+// The plan's costs, those of a tile of codes and of a slot's in the proportion of the newest chunk's keys.
+FcAttendPlan plan_of(const FcAttendArgs& a, int L_clean, bool may_split) {
+    const double slots = (double)a.A * a.L_c, f = L_clean / (L_clean + slots);
+    auto mix = [&](double of_codes, double of_rows) { return f * of_codes + (1.0 - f) * of_rows; };
+    return fc_attend_plan(a.A, a.L_c, L_clean, a.H_q, may_split, a.d == 128 ? FcAttendCosts{mix(4.7, 9.0), 8.0, 5.0, 16.0, 0.5, mix(0.32, 0.65), 10, true}
+                                                                            : FcAttendCosts{mix(3.2, 5.2), 6.0, 5.0, 8.0, 0.5, mix(0.20, 0.40), 14, true});
 }
 
 template <int D>
@@ -295,7 +626,14 @@ int launch(FcAttendArgs a, const FcKv4& x, hipStream_t s) {
     a.L_clean = 0;                    // the slots alone
     FcAttendPlan p = plan_of(a, x.L_clean, true);
     if (!fc_room_for_partials(a.ws, a.ws_bytes, p.parts, D)) p = plan_of(a, x.L_clean, false);
-    attend_kv4_f32_kernel<D><<<p.grid, NT, 0, s>>>(a, p, (float*)a.ws, x);
+    bool wide = false, narrow = false;
+    for (int R = 0; R < a.A; ++R) (p.narrow[R] ? narrow : wide) = true;
+    if (!narrow)
+        attend_kv4_f32_kernel<D, true, false><<<p.grid, NT, 0, s>>>(a, p, (float*)a.ws, x);
+    else if (!wide)
+        attend_kv4_f32_kernel<D, false, true><<<p.grid, NT, 0, s>>>(a, p, (float*)a.ws, x);
+    else
+        attend_kv4_f32_kernel<D, true, true><<<p.grid, NT, 0, s>>>(a, p, (float*)a.ws, x);
     FC_LAUNCH_CHECK();
     return launch_merge4<float, D>(a, p, s);
 }

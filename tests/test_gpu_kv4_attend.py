@@ -141,6 +141,17 @@ def test_lists(idx, n, rec, L_c, dtype):
     check(4, 2, 64, 3, L_c, 100, rec, idx=idx, n=n, dtype=dtype)
 
 
+@pytest.mark.parametrize("H_q,H_k,d", [(1, 1, 128), (2, 1, 64)])
+@pytest.mark.parametrize("L_clean", [0, 1, 31, 32, 33, 650, 5000])
+@pytest.mark.parametrize("rec", [(0, 1, 2), (2, 0), (1,)])
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32])
+def test_many_rows(H_q, H_k, d, L_clean, rec, dtype):
+    """256-row blocks: tiles of codes alone, the last of them before a slot's, slots alone; keys in ranges and, without room, whole."""
+    check(H_q, H_k, d, 3, 1500, L_clean, rec, seed=L_clean, grow=L_clean == 650, reverse=len(rec) == 2, dtype=dtype)
+    if len(rec) == 3:
+        check(H_q, H_k, d, 3, 1500, L_clean, rec, seed=L_clean + 1, ws=256, dtype=dtype)
+
+
 def test_an_entry_that_is_no_chunk_is_skipped():
     q, bufs, cap4, slots = make(4, 2, 64, 3, 50, 130, 5)
     off, outs = [0, 50, 100], []
