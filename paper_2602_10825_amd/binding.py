@@ -10,6 +10,7 @@ from __future__ import annotations
 
 import ctypes
 import os
+import struct
 from typing import Dict, Optional, Sequence
 
 import torch
@@ -462,12 +463,16 @@ def _same_device(call: str, stream, *tensors: Optional[torch.Tensor]) -> None:
 
 
 _PAIRINGS = {"interleaved": 0, "halves": 1}
-_Three = ctypes.c_int32 * 3
+
+def _ints(xs: Sequence[int]) -> bytes:
+    """Host int32 for the length of a call (half the time of an array of ctypes)."""
+    return struct.pack(f"{len(xs)}i", *xs)
+
 
 
 def _heads_of_rows(call: str, name: str, x: torch.Tensor, rows: int, heads: int, d: int, dtype) -> int:
     """Elements from row to row of ``[rows, heads, d]``, whose heads and elements follow each other."""
-    if tuple(x.shape) != (rows, heads, d) or x.dtype != dtype:
+    if x.shape != (rows, heads, d) or x.dtype != dtype:
         raise ValueError(f"{call}: {name} is [{rows}, {heads}, {d}] of {dtype}, got {tuple(x.shape)} of {x.dtype}")
     row, head, one = x.stride()
     if one != 1 or (heads > 1 and head != d):
@@ -506,19 +511,18 @@ def flowcache_qk_norm_rope(q: torch.Tensor, k: torch.Tensor, v: Optional[torch.T
             raise ValueError(f"{call}: k and v have the same row stride")
         assert v_cache.stride() == strides and v_cache.shape == k_cache.shape and v_cache.dtype == dtype
     for w in (q_weight, k_weight):
-        if w is not None and (w.dtype != torch.float32 or tuple(w.shape) != (d,) or not w.is_contiguous()):
+        if w is not None and (w.dtype != torch.float32 or w.shape != (d,) or not w.is_contiguous()):
             raise ValueError(f"{call}: weights are float32 [{d}]")
     if q_out is None:
         q_out = _empty((rows, H_q, d), dtype, q.device, stream)
     else:
         assert q_out.shape == q.shape and q_out.is_contiguous() and q_out.dtype == dtype
-    per_chunk = ctypes.c_int32 * A
     st = (_lib or lib()).flowcache_qk_norm_rope(
-        _ptr(q), qs, _ptr(k), _ptr(v), ks, _dtype_code(k_cache), H_q, H_k, d, int(norm_eps is not None),
-        0.0 if norm_eps is None else float(norm_eps), _ptr(q_weight), _ptr(k_weight), _Three(*map(int, dims)),
-        _PAIRINGS[pairing], float(theta), int(grid[0]), int(grid[1]), per_chunk(*map(int, frame0)), int(L_c),
-        int(L_clean), A, per_chunk(*map(int, active_off)), _ptr(recompute_idx), _ptr(n_recompute), _ptr(q_out),
-        _ptr(k_cache), _ptr(v_cache), strides[0], strides[1], capacity, _stream(stream))
+        q.data_ptr(), qs, k.data_ptr(), _ptr(v), ks, _dtype_code(k_cache), H_q, H_k, d, int(norm_eps is not None),
+        0.0 if norm_eps is None else float(norm_eps), _ptr(q_weight), _ptr(k_weight), _ints(dims),
+        _PAIRINGS[pairing], float(theta), int(grid[0]), int(grid[1]), _ints(frame0), int(L_c),
+        int(L_clean), A, _ints(active_off), recompute_idx.data_ptr(), n_recompute.data_ptr(),
+        q_out.data_ptr(), k_cache.data_ptr(), _ptr(v_cache), strides[0], strides[1], capacity, _stream(stream))
     _check(call, st)
     return q_out
 
@@ -604,7 +608,7 @@ def flowcache_attend_kv4(q: torch.Tensor, k_new: Optional[torch.Tensor], v_new: 
         workspace = _workspace(L.flowcache_attend_kv4_workspace(A, L_c, H_q, d), q.device, stream)
     st = L.flowcache_attend_kv4(_ptr(q), _ptr(k_new), _ptr(v_new), _ptr(k4), _ptr(v4), int(capacity4), _ptr(k_cache),
                                 _ptr(v_cache), strides[0], strides[1], capacity, _dtype_code(q), H_q, H_k, d, int(L_c),
-                                int(L_clean), A, (ctypes.c_int32 * A)(*map(int, active_off)), _ptr(recompute_idx),
+                                int(L_clean), A, _ints(active_off), _ptr(recompute_idx),
                                 _ptr(n_recompute), float(softmax_scale), _ptr(out), _ptr(lse), _ptr(workspace),
                                 workspace.numel(), _stream(stream))
     _check(call, st)
