@@ -6,7 +6,8 @@ Tolerance.  A weight is rounded to bf16, half a step of 2^-8, and so is its shar
 
 fp32, in units of 2^-24.  A score is 24 (a slot's key 48) additions of products that are exact to 1: 48 B, B the largest sum of
 |q k| times the scale that the row sees; twice that for weight and sum.  Exponential, weight's parts and reference 16.  The row's sums over the
-tiles of one wavefront, 12 additions each of 32 keys, and the merge of 8 wavefronts and up to 32 ranges 40: all times sum p |v|."""
+tiles of one wavefront, an 8th of them, 12 additions each of 32 keys, and the merge of 8 wavefronts and up to 32 ranges 40 (256-row
+blocks: one addition per tile, of all tiles, and 12 within a tile, which is less): all times sum p |v|."""
 import numpy as np
 import pytest
 import torch
