@@ -52,18 +52,20 @@ __device__ __forceinline__ int fc_swapped(int row, int piece) {
 
 namespace {
 
-// The S <= MOST partials of every 32-row unit -> out and lse, as attend_merge_kernel does it but for few rows: a thread has four
-// columns of one row, the factors of a row are computed once, and all of a row's partials are asked for at once, before those
-// (12 x 128, one row on 61201 keys in 20 ranges 15.2 -> 6.4 us; 256 rows on 49201 in 20 ranges 17.9 -> 10.6).
+// The partials of every 32-row unit -> out and lse, as attend_merge_kernel does it but for few rows: a thread has four columns of
+// one row and PER of its ranges, every G-th, whose partials, maxima and sums it asks for at once; the G threads of a column put theirs
+// together in LDS.  (All ranges in one thread, 32 of them unrolled: the loads and the code itself, fetched once per launch, take
+// longer, 12 x 128, one row on 61201 keys in 20 ranges 6.4 us instead of 3.7)
 constexpr int kMergeThreads = 256;
-template <int D>
+template <int D, int G>
 struct MergeShape {
-    static constexpr int TPR = D / 4, RPB = kMergeThreads / TPR, BPU = kUnitRows / RPB;   // threads per row, rows per block, blocks per unit
+    static constexpr int TPR = D / 4, RPB = kMergeThreads / (TPR * G), BPU = kUnitRows / RPB;   // threads per row and group, rows per block, blocks per unit
 };
-template <typename T, int D, int MOST>
+template <typename T, int D, int PER, int G>
 __global__ __launch_bounds__(kMergeThreads) void merge4_kernel(FcAttendArgs a, FcAttendPlan p, const float* parts) {
-    constexpr int TPR = MergeShape<D>::TPR, RPB = MergeShape<D>::RPB, BPU = MergeShape<D>::BPU;
-    __shared__ float m_s[MOST][RPB], l_s[MOST][RPB];
+    constexpr int TPR = MergeShape<D, G>::TPR, RPB = MergeShape<D, G>::RPB, BPU = MergeShape<D, G>::BPU;
+    __shared__ __attribute__((aligned(16))) float4 acc_s[G][RPB][TPR];
+    __shared__ float m_s[G][RPB], l_s[G][RPB];
     const uint32_t valid = valid_blocks(a);
     const int R = __popc(valid);
     if (R == 0) return;
@@ -74,46 +76,60 @@ __global__ __launch_bounds__(kMergeThreads) void merge4_kernel(FcAttendArgs a, F
     if (!merge_unit(a, p, valid, R, S, unit, tile, r, h)) return;
     const int first_row = tile * kUnitRows + row0;
     if (first_row >= a.L_c) return;
-    const int row = threadIdx.x / TPR, c0 = threadIdx.x % TPR * 4;
-    const float4* src = reinterpret_cast<const float4*>(parts + ((int64_t)unit * S * kUnitRows + row0 + row) * D + c0);
-    float4 v[MOST];
+    const int row = threadIdx.x / (TPR * G), g = threadIdx.x / TPR % G, c = threadIdx.x % TPR;
+    const float4* src = reinterpret_cast<const float4*>(parts + ((int64_t)unit * S * kUnitRows + row0 + row) * D) + c;
+    const float* ml = parts + (int64_t)p.parts * kUnitRows * D + (int64_t)unit * S * 2 * kUnitRows + row0 + row;
+    float4 v[PER];
+    float m[PER], l_of[PER];
 #pragma unroll
-    for (int s = 0; s < MOST; ++s) v[s] = src[(int64_t)(s < S ? s : S - 1) * (kUnitRows * D / 4)];
-    const float* ml = parts + (int64_t)p.parts * kUnitRows * D + (int64_t)unit * S * 2 * kUnitRows + row0;
-    for (int i = threadIdx.x; i < S * RPB; i += kMergeThreads) {
-        m_s[i / RPB][i % RPB] = ml[i / RPB * 2 * kUnitRows + i % RPB];
-        l_s[i / RPB][i % RPB] = ml[(i / RPB * 2 + 1) * kUnitRows + i % RPB];
+    for (int e = 0; e < PER; ++e) {
+        const int s = g + e * G < S ? g + e * G : S - 1;
+        v[e] = src[(int64_t)s * (kUnitRows * D / 4)];
+        m[e] = ml[s * 2 * kUnitRows];
+        l_of[e] = ml[(s * 2 + 1) * kUnitRows];
     }
-    __syncthreads();
-    float mt = kNegBig;
+    float mt = kNegBig, l = 0.f;
 #pragma unroll
-    for (int s = 0; s < MOST; ++s) mt = fmaxf(mt, s < S ? m_s[s][row] : kNegBig);
-    float acc[4] = {0.f, 0.f, 0.f, 0.f}, l = 0.f;
+    for (int e = 0; e < PER; ++e) mt = fmaxf(mt, m[e]);       // (the last range's, again, where there is none)
+    float4 acc = make_float4(0.f, 0.f, 0.f, 0.f);
+    auto add = [&](const float4& x, float lx, float f) {
+        l = fmaf(lx, f, l);
+        acc.x = fmaf(x.x, f, acc.x); acc.y = fmaf(x.y, f, acc.y); acc.z = fmaf(x.z, f, acc.z); acc.w = fmaf(x.w, f, acc.w);
+    };
 #pragma unroll
-    for (int s = 0; s < MOST; ++s) {
-        const float f = s < S ? __builtin_amdgcn_exp2f(m_s[s][row] - mt) : 0.f;
-        l = fmaf(s < S ? l_s[s][row] : 0.f, f, l);
-        acc[0] = fmaf(v[s].x, f, acc[0]);
-        acc[1] = fmaf(v[s].y, f, acc[1]);
-        acc[2] = fmaf(v[s].z, f, acc[2]);
-        acc[3] = fmaf(v[s].w, f, acc[3]);
+    for (int e = 0; e < PER; ++e) add(v[e], l_of[e], g + e * G < S ? __builtin_amdgcn_exp2f(m[e] - mt) : 0.f);
+    if (G > 1) {
+        acc_s[g][row][c] = acc;
+        if (c == 0) { m_s[g][row] = mt; l_s[g][row] = l; }
+        __syncthreads();
+        if (g > 0) return;
+#pragma unroll
+        for (int o = 1; o < G; ++o) mt = fmaxf(mt, m_s[o][row]);
+        acc = make_float4(0.f, 0.f, 0.f, 0.f);
+        l = 0.f;
+#pragma unroll
+        for (int o = 0; o < G; ++o) add(acc_s[o][row][c], l_s[o][row], __builtin_amdgcn_exp2f(m_s[o][row] - mt));
     }
     if (first_row + row >= a.L_c) return;
     const float inv = 1.0f / l;
     const int64_t grow = (int64_t)r * a.L_c + first_row + row;
-    store_out((T*)a.out + (grow * a.H_q + h) * D + c0, acc[0] * inv, acc[1] * inv, acc[2] * inv, acc[3] * inv);
-    if (a.lse && c0 == 0) a.lse[(int64_t)h * a.A * a.L_c + grow] = (mt + __builtin_amdgcn_logf(l)) * 0.6931471805599453f;
+    store_out((T*)a.out + (grow * a.H_q + h) * D + 4 * c, acc.x * inv, acc.y * inv, acc.z * inv, acc.w * inv);
+    if (a.lse && c == 0) a.lse[(int64_t)h * a.A * a.L_c + grow] = (mt + __builtin_amdgcn_logf(l)) * 0.6931471805599453f;
 }
 
+template <typename T, int D, int PER, int G>
+void merge4(const FcAttendArgs& a, const FcAttendPlan& p, hipStream_t s) {
+    merge4_kernel<T, D, PER, G><<<p.merge_grid * MergeShape<D, G>::BPU, kMergeThreads, 0, s>>>(a, p, (const float*)a.ws);
+}
 template <typename T, int D>
 int launch_merge4(const FcAttendArgs& a, const FcAttendPlan& p, hipStream_t s) {
     if (p.merge_grid == 0) return FC_OK;
-    const dim3 grid(p.merge_grid * MergeShape<D>::BPU);
     int most = 1;
     for (int R = 0; R < a.A; ++R) most = p.splits[R] > most ? p.splits[R] : most;
-    if (most <= 4) merge4_kernel<T, D, 4><<<grid, kMergeThreads, 0, s>>>(a, p, (const float*)a.ws);
-    else if (most <= 12) merge4_kernel<T, D, 12><<<grid, kMergeThreads, 0, s>>>(a, p, (const float*)a.ws);
-    else merge4_kernel<T, D, kMaxSplits><<<grid, kMergeThreads, 0, s>>>(a, p, (const float*)a.ws);
+    static_assert(kMaxSplits <= 32, "8 ranges for each of 4 threads");
+    if (most <= 4) merge4<T, D, 4, 1>(a, p, s);
+    else if (most <= 12) merge4<T, D, 3, 4>(a, p, s);
+    else merge4<T, D, 8, 4>(a, p, s);
     FC_LAUNCH_CHECK();
     return FC_OK;
 }
