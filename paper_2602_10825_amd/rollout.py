@@ -9,13 +9,13 @@ What is real is every FlowCache step, which runs in the library's kernels on dev
 decisions.  ``run_rollout`` returns per-tick decisions, per-commit kept indices (optionally)
 and timing / work totals, so that a thresholded run can be set beside the eps = 0 run.
 
-    python -m paper_2602_10825_amd.rollout --layers 4 --units 6 --steps 12
+    python -m paper_2602_10825_amd.rollout --layers 4 --units 6 --steps 12 --stagger 6
 
 With ``grid`` the queries and keys go through a per-head norm and the rotation by (time, height, width) on their
 way out of the projection; with ``kv4`` the clean regions are held in 4 bits (a layer's cache then holds the
 active chunks' slots alone, and one scratch cache serves the commits of all layers):
 
-    python -m paper_2602_10825_amd.rollout --layers 4 --units 6 --steps 12 --grid 34x60 --kv4
+    python -m paper_2602_10825_amd.rollout --layers 4 --units 6 --steps 12 --stagger 6 --grid 34x60 --kv4
 """
 from __future__ import annotations
 
