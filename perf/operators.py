@@ -138,7 +138,7 @@ def _to4(x):
     a = torch.ldexp(b, -e)
     s = a.abs()
     code = ((s > .25).to(torch.uint8) + (s >= .75) + (s > 1.25) + (s >= 1.75) + (s > 2.5) + (s >= 3.5) + (s > 5.)
-            + 8 * (a < 0).to(torch.uint8)).view(H, n, d // 2, 2)
+            + 8 * (a < 0)).view(H, n, d // 2, 2)
     return torch.cat(((code[..., 0] | code[..., 1] << 4).reshape(-1), (e + 127).to(torch.uint8).reshape(-1)))
 
 
@@ -250,11 +250,17 @@ def _run_pack(s, c):
     return {"k": s["k_back"], "v": s["v_back"]}
 
 
+def _bytes(s):
+    """The 4-bit buffers as the calls take them.  _to4() leaves whole numbers of 64 bits, so a pass also reads 8 bytes and
+    writes one for each byte that the call itself reads."""
+    return s["k4"].to(torch.uint8), s["v4"].to(torch.uint8)
+
+
 def _run_unpack(s, c):
     n = c["count"]
     if own:
         from paper_2602_10825_amd import binding as B
-        B.flowcache_kv4_unpack(s["k4"], s["v4"], c["L"], s["k_back"], s["v_back"], n)
+        B.flowcache_kv4_unpack(*_bytes(s), c["L"], s["k_back"], s["v_back"], n)
     else:
         s["k_back"].copy_(_values(s["k4"], c["H"], c["L"], c["d"])[:, :n])
         s["v_back"].copy_(_values(s["v4"], c["H"], c["L"], c["d"])[:, :n])
@@ -265,7 +271,7 @@ def _run_attend(s, c):
     H_q, H_k, d, A, R, L_c, L = c["H_q"], c["H_k"], c["d"], c["A"], c["R"], c["L_c"], c["L_clean"]
     if own:
         from paper_2602_10825_amd import binding as B
-        return B.flowcache_attend_kv4(s["q"], None, None, s["k4"], s["v4"], L, s["k_cache"], s["v_cache"], L_c, L, s["off"],
+        return B.flowcache_attend_kv4(s["q"], None, None, *_bytes(s), L, s["k_cache"], s["v_cache"], L_c, L, s["off"],
                                       s["idx"], s["n"], out=s["out"], want_lse=False)["out"]
     rows, group = R * L_c, H_q // H_k
     k = torch.cat((_values(s["k4"], H_k, L, d), s["k_cache"].float()), 1)
