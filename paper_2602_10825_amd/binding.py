@@ -595,7 +595,7 @@ def flowcache_attend_kv4(q: torch.Tensor, k_new: Optional[torch.Tensor], v_new: 
         assert x is None or (x.is_contiguous() and x.shape == (rows, H_k, d) and x.dtype == q.dtype)
     if k4 is None:
         strides = k_cache.stride()
-        assert strides[2] == 1 and v_cache.stride() == strides and v_cache.shape == k_cache.shape
+        assert strides[2] == 1 and v_cache.stride() == strides and v_cache.shape == k_cache.shape and v_cache.dtype == k_cache.dtype
     else:
         strides = _kv4_shapes(call, k4, v4, capacity4, k_cache, v_cache)
     if out is None:

@@ -1,0 +1,52 @@
+"""What the Python calls refuse before the library is asked: tensors whose type would be misread.  CPU only; the library
+is stood in for, so a call that is let through shows as one and touches nothing."""
+import pytest
+import torch
+
+from paper_2602_10825_amd import binding as B
+
+BF, F32, I32 = torch.bfloat16, torch.float32, torch.int32
+
+
+class LetThrough(Exception):
+    pass
+
+
+class Library:
+    """Answers the size queries; any other call has been let through."""
+
+    def __getattr__(self, name):
+        if name.endswith("_workspace"):
+            return lambda *a: 256
+
+        def call(*a):
+            raise LetThrough(name)
+        return call
+
+
+@pytest.fixture(autouse=True)
+def stand_in(monkeypatch):
+    monkeypatch.setattr(B, "_lib", Library())
+    monkeypatch.setattr(B, "_same_device", lambda *a: None)
+    monkeypatch.setattr(B, "_stream", lambda stream: 0)
+
+
+def z(*shape, dtype=BF):
+    return torch.zeros(shape, dtype=dtype)
+
+
+def attend(**kw):
+    args = dict(q=z(16, 4, 64), k_new=None, v_new=None, k4=None, v4=None, capacity4=0, k_cache=z(2, 16, 64), v_cache=z(2, 16, 64),
+                L_c=8, L_clean=0, active_off=[0, 8], recompute_idx=z(2, dtype=I32), n_recompute=z(1, dtype=I32))
+    return B.flowcache_attend_kv4(**{**args, **kw})
+
+
+def test_valid_calls_are_let_through():
+    with pytest.raises(LetThrough):
+        attend()
+
+
+@pytest.mark.parametrize("k,v", [(F32, BF), (BF, F32)])
+def test_attention_without_clean_rows_wants_one_type_for_both_caches(k, v):
+    with pytest.raises(AssertionError):
+        attend(q=z(16, 4, 64, dtype=k), k_cache=z(2, 16, 64, dtype=k), v_cache=z(2, 16, 64, dtype=v))
