@@ -462,6 +462,13 @@ def _same_device(call: str, stream, *tensors: Optional[torch.Tensor]) -> None:
             raise ValueError(f"{call}: a tensor on {t.device}, the stream on cuda:{on}")
 
 
+def _check_lists(call: str, recompute_idx: torch.Tensor, n_recompute: torch.Tensor) -> None:
+    """The kernels read the recompute list by address: entries of another type would be other chunks."""
+    for x in (recompute_idx, n_recompute):
+        if x.dtype != torch.int32 or not x.is_contiguous():
+            raise ValueError(f"{call}: recompute_idx and n_recompute are contiguous int32, got strides {x.stride()} of {x.dtype}")
+
+
 _PAIRINGS = {"interleaved": 0, "halves": 1}
 
 def _ints(xs: Sequence[int]) -> bytes:
@@ -502,6 +509,7 @@ def flowcache_qk_norm_rope(q: torch.Tensor, k: torch.Tensor, v: Optional[torch.T
     if pairing not in _PAIRINGS:
         raise ValueError(f"{call}: pairing is one of {sorted(_PAIRINGS)}, got {pairing!r}")
     _same_device(call, stream, q, k, v, k_cache, v_cache, recompute_idx, n_recompute, q_weight, k_weight, q_out)
+    _check_lists(call, recompute_idx, n_recompute)
     qs = _heads_of_rows(call, "q", q, rows, H_q, d, dtype)
     ks = _heads_of_rows(call, "k", k, rows, H_k, d, dtype)
     strides = k_cache.stride()
@@ -589,6 +597,7 @@ def flowcache_attend_kv4(q: torch.Tensor, k_new: Optional[torch.Tensor], v_new: 
     H_k, capacity, _ = k_cache.shape
     A = len(active_off)
     _same_device(call, stream, q, k_cache, v_cache, k_new, v_new, k4, v4, recompute_idx, n_recompute, out, workspace)
+    _check_lists(call, recompute_idx, n_recompute)
     assert q.is_contiguous() and rows == A * L_c and k_cache.shape[2] == d and (k4 is None) == (v4 is None)
     assert q.dtype == k_cache.dtype and v_cache is not None
     for x in (k_new, v_new):

@@ -50,3 +50,23 @@ def test_valid_calls_are_let_through():
 def test_attention_without_clean_rows_wants_one_type_for_both_caches(k, v):
     with pytest.raises(AssertionError):
         attend(q=z(16, 4, 64, dtype=k), k_cache=z(2, 16, 64, dtype=k), v_cache=z(2, 16, 64, dtype=v))
+
+
+def rope(**kw):
+    args = dict(q=z(16, 4, 64), k=z(16, 2, 64), v=z(16, 2, 64), k_cache=z(2, 16, 64), v_cache=z(2, 16, 64), L_c=8, L_clean=0,
+                active_off=[0, 8], recompute_idx=z(2, dtype=I32), n_recompute=z(1, dtype=I32), dims=(24, 20, 20), grid=(2, 4), frame0=[0, 1])
+    return B.flowcache_qk_norm_rope(**{**args, **kw})
+
+
+@pytest.mark.parametrize("call", [attend, rope])
+@pytest.mark.parametrize("bad", [dict(recompute_idx=z(2, dtype=torch.int64)), dict(n_recompute=z(1, dtype=torch.int64)),
+                                 dict(recompute_idx=z(2, dtype=F32)), dict(n_recompute=z(1, dtype=torch.uint8)),
+                                 dict(recompute_idx=z(4, dtype=I32)[::2])])
+def test_recompute_lists_are_int32_and_without_gaps(call, bad):
+    """Two entries 0, 1 of 64 bits would be read as chunks 0, 0: two row blocks for one slot."""
+    with pytest.raises(LetThrough):
+        call()
+    with pytest.raises(LetThrough):
+        call(n_recompute=torch.tensor(1, dtype=I32))               # a number without dimensions is one entry
+    with pytest.raises(ValueError):
+        call(**bad)
