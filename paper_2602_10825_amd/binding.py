@@ -462,6 +462,12 @@ def _same_device(call: str, stream, *tensors: Optional[torch.Tensor]) -> None:
             raise ValueError(f"{call}: a tensor on {t.device}, the stream on cuda:{on}")
 
 
+def _check_ints(call: str, *xs: int) -> None:
+    """The library takes them as int: what lies beyond would be cut to 32 bits."""
+    if max(xs) > 0x7fffffff or min(xs) < -0x80000000:
+        raise ValueError(f"{call}: a number beyond 32 bits among {xs}")
+
+
 def _check_lists(call: str, recompute_idx: torch.Tensor, n_recompute: torch.Tensor) -> None:
     """The kernels read the recompute list by address: entries of another type would be other chunks."""
     for x in (recompute_idx, n_recompute):
@@ -510,6 +516,7 @@ def flowcache_qk_norm_rope(q: torch.Tensor, k: torch.Tensor, v: Optional[torch.T
         raise ValueError(f"{call}: pairing is one of {sorted(_PAIRINGS)}, got {pairing!r}")
     _same_device(call, stream, q, k, v, k_cache, v_cache, recompute_idx, n_recompute, q_weight, k_weight, q_out)
     _check_lists(call, recompute_idx, n_recompute)
+    _check_ints(call, L_clean, *grid)
     qs = _heads_of_rows(call, "q", q, rows, H_q, d, dtype)
     ks = _heads_of_rows(call, "k", k, rows, H_k, d, dtype)
     strides = k_cache.stride()
@@ -537,6 +544,7 @@ def flowcache_qk_norm_rope(q: torch.Tensor, k: torch.Tensor, v: Optional[torch.T
 
 def kv4_buffer(H_k: int, capacity4: int, d: int, device="cuda") -> torch.Tensor:
     """A buffer for ``capacity4`` rows per head of K or V in 4 bits."""
+    _check_ints("flowcache_kv4_bytes", H_k, capacity4, d)
     nbytes = (_lib or lib()).flowcache_kv4_bytes(int(H_k), int(capacity4), int(d))
     if nbytes == 0:
         raise FlowCacheError("flowcache_kv4_bytes", FC_INVALID_ARGUMENT)
@@ -562,6 +570,7 @@ def flowcache_kv4_pack(k_cache: torch.Tensor, v_cache: Optional[torch.Tensor], k
     call = "flowcache_kv4_pack"
     H_k, capacity, d = k_cache.shape
     _same_device(call, stream, k_cache, v_cache, k4, v4, kept_idx)
+    _check_ints(call, capacity4, count, cache_pos, pos4)
     strides = _kv4_shapes(call, k4, v4, capacity4, k_cache, v_cache)
     assert kept_idx is None or (kept_idx.dtype == torch.int32 and kept_idx.is_contiguous() and kept_idx.shape == (H_k, count))
     st = (_lib or lib()).flowcache_kv4_pack(_ptr(k_cache), _ptr(v_cache), strides[0], strides[1], capacity,
@@ -577,6 +586,7 @@ def flowcache_kv4_unpack(k4: torch.Tensor, v4: Optional[torch.Tensor], capacity4
     call = "flowcache_kv4_unpack"
     H_k, capacity, d = k_cache.shape
     _same_device(call, stream, k_cache, v_cache, k4, v4)
+    _check_ints(call, capacity4, count, cache_pos, pos4)
     strides = _kv4_shapes(call, k4, v4, capacity4, k_cache, v_cache)
     st = (_lib or lib()).flowcache_kv4_unpack(_ptr(k4), _ptr(v4), int(capacity4), int(pos4), int(count), _ptr(k_cache),
                                               _ptr(v_cache), strides[0], strides[1], capacity, _dtype_code(k_cache),
@@ -598,6 +608,7 @@ def flowcache_attend_kv4(q: torch.Tensor, k_new: Optional[torch.Tensor], v_new: 
     A = len(active_off)
     _same_device(call, stream, q, k_cache, v_cache, k_new, v_new, k4, v4, recompute_idx, n_recompute, out, workspace)
     _check_lists(call, recompute_idx, n_recompute)
+    _check_ints(call, L_clean, capacity4)
     assert q.is_contiguous() and rows == A * L_c and k_cache.shape[2] == d and (k4 is None) == (v4 is None)
     assert q.dtype == k_cache.dtype and v_cache is not None
     for x in (k_new, v_new):

@@ -70,3 +70,31 @@ def test_recompute_lists_are_int32_and_without_gaps(call, bad):
         call(n_recompute=torch.tensor(1, dtype=I32))               # a number without dimensions is one entry
     with pytest.raises(ValueError):
         call(**bad)
+
+
+def pack(**kw):
+    args = dict(k_cache=z(2, 16, 64), v_cache=None, k4=z(2 * 16 * 34, dtype=torch.uint8), v4=None, capacity4=16, count=4, cache_pos=1, pos4=2)
+    return B.flowcache_kv4_pack(**{**args, **kw})
+
+
+def unpack(**kw):
+    args = dict(k4=z(2 * 16 * 34, dtype=torch.uint8), v4=None, capacity4=16, k_cache=z(2, 16, 64), v_cache=None, count=4, cache_pos=1, pos4=2)
+    return B.flowcache_kv4_unpack(**{**args, **kw})
+
+
+@pytest.mark.parametrize("call,names", [(pack, ("count", "cache_pos", "pos4")), (unpack, ("count", "cache_pos", "pos4")),
+                                        (attend, ("L_clean", "capacity4")), (rope, ("L_clean",))])
+@pytest.mark.parametrize("more", [1 << 32, -(1 << 32), 1 << 40])
+def test_numbers_beyond_32_bits_are_refused(call, names, more):
+    """The library takes them as int: 2^32 + 3 rows would be 3."""
+    with pytest.raises(LetThrough):
+        call()
+    for name in names:
+        with pytest.raises(ValueError):
+            call(**{name: more + 3})
+
+
+def test_a_frame_beyond_32_bits_is_refused():
+    for grid in ((1 << 32, 4), (2, (1 << 32) + 4)):
+        with pytest.raises(ValueError):
+            rope(grid=grid)
