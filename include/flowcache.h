@@ -389,8 +389,9 @@ size_t flowcache_kv_compress_status_offset(int H_k, int L_k, int d, int budget, 
  * flowcache_attend follows with k_new = v_new = NULL.  q, k and v must not overlap what is written
  * (but for q_out = q).
  * Errors: null pointers, grid_h or grid_w < 1, theta < 1 or not finite, norm_eps < 0 or not finite,
- * dims odd, negative or beyond d, slots outside the cache or overlapping -> FC_INVALID_ARGUMENT; d not in
- * {64, 128}, strides or pointers that are not multiples of 16 bytes, L_c above 2^27 - 8 -> FC_UNSUPPORTED.
+ * dims odd, negative or beyond d, slots outside the cache or overlapping, q_out = q where q's rows have gaps
+ * -> FC_INVALID_ARGUMENT; d not in {64, 128}, strides or pointers that are not multiples of 16 bytes,
+ * L_c above 2^27 - 8 -> FC_UNSUPPORTED.
  */
 typedef enum { FC_ROPE_INTERLEAVED = 0, FC_ROPE_HALVES = 1 } fc_rope_pairing;
 int flowcache_qk_norm_rope(const void* q, int64_t q_tok_stride, const void* k, const void* v,

@@ -299,6 +299,8 @@ int flowcache_qk_norm_rope(const void* q, int64_t q_tok_stride, const void* k, c
     if (q_tok_stride < (int64_t)H_q * d || kv_new_tok_stride < (int64_t)H_k * d) return FC_INVALID_ARGUMENT;
     if (q_tok_stride % per16 != 0 || kv_new_tok_stride % per16 != 0) return FC_UNSUPPORTED;
     if (!aligned16(q) || !aligned16(k) || !aligned16(v) || !aligned16(q_out)) return FC_UNSUPPORTED;
+    // (in place over rows with gaps, one block's output would lie on rows that another has yet to read)
+    if (q_out == q && (int64_t)A * L_c > 1 && q_tok_stride != (int64_t)H_q * d) return FC_INVALID_ARGUMENT;
     if (L_c > kMostRows || (int64_t)A * L_c > INT32_MAX || (int64_t)grid_h * grid_w > INT32_MAX) return FC_UNSUPPORTED;
 
     FcRopeArgs a{};
