@@ -4,6 +4,7 @@
 #include <cstring>
 
 #include "fc_common.hpp"
+#include "rope_turns.hpp"
 
 namespace {
 
@@ -311,13 +312,7 @@ int flowcache_qk_norm_rope(const void* q, int64_t q_tok_stride, const void* k, c
     a.q_weight = norm ? q_weight : nullptr; a.k_weight = norm ? k_weight : nullptr; a.eps = norm_eps; a.norm = norm; a.pairing = pairing;
     a.grid_h = grid_h; a.grid_w = grid_w;
     a.pairs_t = dims[0] / 2; a.pairs_th = (dims[0] + dims[1]) / 2;
-    // theta^(-2 i / dims) by repeated products: at most 64 roundings to 64 bits instead of as many powers (3 us of a call)
-    for (int axis = 0, p = 0; axis < 3; ++axis) {
-        if (dims[axis] == 0) continue;
-        const double ratio = std::pow(theta, -2.0 / dims[axis]);
-        double turns = 1.0 / (2.0 * M_PI);
-        for (int i = 0; i < dims[axis] / 2; ++i, turns *= ratio) a.turns[p++] = turns;
-    }
+    fc_rope_turns(theta, dims, a.turns, a.turns_rest);
     std::memcpy(a.frame0, frame0, sizeof(int32_t) * A);
     std::memcpy(a.active_off, active_off, sizeof(int32_t) * A);
     a.rec_idx = recompute_idx; a.n_rec = n_recompute;

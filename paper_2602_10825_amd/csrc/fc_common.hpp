@@ -144,7 +144,7 @@ struct FcRopeArgs {
     fc_dtype dtype; int H_q, H_k, d, L_c, A;
     const float* q_weight; const float* k_weight; float eps; int norm, pairing;
     int grid_h, grid_w, pairs_t, pairs_th;       // pairs [0, pairs_t) turn with time, [pairs_t, pairs_th) with height
-    double turns[64];                            // revolutions per unit of position; 0: a pair that does not turn
+    double turns[64]; float turns_rest[64];      // revolutions per unit of position, in two parts; 0: a pair that does not turn
     int32_t frame0[FC_MAX_ACTIVE], active_off[FC_MAX_ACTIVE];
     const int32_t* rec_idx; const int32_t* n_rec;
 };

@@ -91,9 +91,11 @@ __global__ __launch_bounds__(kThreads) void qk_norm_rope_kernel(FcRopeArgs a, in
 #pragma unroll
         for (int i = 0; i < NP; ++i) {
             const int p = l * NP + i;
-            // in revolutions: whole ones are dropped in 64 bits, so far positions lose nothing
-            const double t = (p < a.pairs_t ? pt : p < a.pairs_th ? ph : pw) * a.turns[p];
-            sincospif(2.0f * (float)(t - rint(t)), &sn[i], &cs[i]);
+            // In revolutions, whole ones dropped before anything is rounded (turns and turns_rest: rope_turns.hpp), so far positions lose
+            // nothing: with turns alone, frame 2^31 is off by 8 units of 2^-24.
+            const double pos = p < a.pairs_t ? pt : p < a.pairs_th ? ph : pw, turns = a.turns[p];
+            const double t = fma(pos, turns, -rint(pos * turns)) + pos * a.turns_rest[p];
+            sincospif(2.0f * (float)t, &sn[i], &cs[i]);
             wq[P::first(i)] = a.q_weight ? a.q_weight[P::first_at(l, i)] : 1.0f;
             wq[P::second(i)] = a.q_weight ? a.q_weight[P::second_at(l, i)] : 1.0f;
             wk[P::first(i)] = a.k_weight ? a.k_weight[P::first_at(l, i)] : 1.0f;
