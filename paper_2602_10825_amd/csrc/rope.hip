@@ -27,6 +27,21 @@ __device__ __forceinline__ float group_sum(float v) {
     return v;
 }
 
+// Heads whose mean square leaves a float's range, or its normal numbers: the elements times a power of two first (small ones), or the
+// root's inverse and then the power (large ones; the other order would lose bits of small elements).  f becomes what the returned
+// factor has yet to be multiplied with.  Rare: a group's lanes agree, so it is a branch that others skip.
+template <int G, int V>
+__device__ __forceinline__ float norm_far(float (&f)[V], bool small, float eps, float inv_d) {
+    const float to = small ? 0x1p100f : 0x1p-68f;
+    float ss = 0.f;
+#pragma unroll
+    for (int i = 0; i < V; ++i) ss = fmaf(f[i] * to, f[i] * to, ss);
+    const float inv = rsqrtf(group_sum<G>(ss) * inv_d + eps * to * to);
+#pragma unroll
+    for (int i = 0; i < V; ++i) f[i] = small ? f[i] * to : f[i] * inv * to;
+    return small ? inv : 1.0f;
+}
+
 // A lane's 16 bytes of a head, as two halves of the pairs' elements: neighbours (HALVES: one from each side of the head).
 template <typename T, int D, bool HALVES>
 struct Part {
@@ -124,7 +139,9 @@ __global__ __launch_bounds__(kThreads) void qk_norm_rope_kernel(FcRopeArgs a, in
                     float ss = 0.f;
 #pragma unroll
                     for (int i = 0; i < P::V; ++i) ss = fmaf(f[i], f[i], ss);
-                    const float inv = rsqrtf(group_sum<G>(ss) * (1.0f / D) + a.eps);
+                    const float ms = group_sum<G>(ss) * (1.0f / D) + a.eps;
+                    float inv = rsqrtf(ms);
+                    if (!(ms >= 0x1p-96f && ms <= 0x1p120f)) inv = norm_far<G>(f, ms < 0x1p-96f, a.eps, 1.0f / D);
 #pragma unroll
                     for (int i = 0; i < P::V; ++i) f[i] = f[i] * inv * (is_q ? wq[i] : wk[i]);
                 }
