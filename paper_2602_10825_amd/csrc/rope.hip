@@ -70,7 +70,9 @@ struct Part {
     static __device__ __forceinline__ int second_at(int l, int i) { return HALVES ? D / 2 + l * NP + i : 2 * (l * NP + i) + 1; }
 };
 __device__ __forceinline__ uint4 pack16(const float (&f)[8], bf16_t) {
-    auto two = [](float x, float y) { return (uint32_t)f32_to_bf16(x) | ((uint32_t)f32_to_bf16(y) << 16); };
+    // (f32_to_bf16() is for finite values: some NaN become zeros there)
+    typedef __bf16 bf16x2_t __attribute__((ext_vector_type(2)));
+    auto two = [](float x, float y) { return __builtin_bit_cast(uint32_t, (bf16x2_t){(__bf16)x, (__bf16)y}); };
     return make_uint4(two(f[0], f[1]), two(f[2], f[3]), two(f[4], f[5]), two(f[6], f[7]));
 }
 __device__ __forceinline__ uint4 pack16(const float (&f)[4], float) {
