@@ -97,7 +97,11 @@ __global__ __launch_bounds__(kMergeThreads) void merge4_kernel(FcAttendArgs a, F
         acc.x = fmaf(x.x, f, acc.x); acc.y = fmaf(x.y, f, acc.y); acc.z = fmaf(x.z, f, acc.z); acc.w = fmaf(x.w, f, acc.w);
     };
 #pragma unroll
-    for (int e = 0; e < PER; ++e) add(v[e], l_of[e], g + e * G < S ? __builtin_amdgcn_exp2f(m[e] - mt) : 0.f);
+    for (int e = 0; e < PER; ++e) {                            // (... and nothing there: it may hold infinities, so no factor of zero)
+        const bool there = g + e * G < S;
+        const float4 x = there ? v[e] : make_float4(0.f, 0.f, 0.f, 0.f);
+        add(x, there ? l_of[e] : 0.f, __builtin_amdgcn_exp2f(m[e] - mt));
+    }
     if (G > 1) {
         acc_s[g][row][c] = acc;
         if (c == 0) { m_s[g][row] = mt; l_s[g][row] = l; }
