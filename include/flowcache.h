@@ -447,10 +447,9 @@ int flowcache_kv4_unpack(const void* k4, const void* v4, int capacity4, int pos4
  * in k_cache / v_cache: active_off may start at 0.  Arguments, errors and workspace as there, and
  *
  *   k4, v4   [dev] buffers of capacity4 rows per head; may be NULL if L_clean = 0.  What the rows that
- *                  are seen stand for has to be finite, as the caches' elements have to be
+ *                  are seen stand for has to be finite
  *   dtype    type of q, the caches and out.  The 4-bit values are operands without rounding, so the result
- *            is flowcache_attend's on the unpacked rows.  fp32 elements of q (times the scale) and of the
- *            slots keep all their bits if they are 0 or from 2^-100 to 2^127 in magnitude
+ *            is flowcache_attend's on the unpacked rows, in fp32 over the whole range of a float
  * More than 2^31 - 257 visible positions or A * H_q * ceil(L_c / 32) of 2^23 - 8 and more -> FC_UNSUPPORTED.
  * The importance mass is not emitted here: at a commit the clean keys are unpacked for the selection
  * anyway, and flowcache_attention_mass takes them from there.

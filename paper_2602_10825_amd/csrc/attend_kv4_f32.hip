@@ -8,8 +8,8 @@
 // The large ones run at 325 .. 380 TFLOP/s counted as fp32, where a third (codes) and a sixth (slots) of a large bf16 product's rate are
 // 394 and 197: matrix cores.
 //
-// Operands are finite; a part is lost below 2^-110, so entries of Q (times the scale) and of the slots hold all their bits from
-// 2^-100 on.
+// What has no parts or loses them (infinities, entries near the largest float, very small ones) is looked for in Q and in the sums, and
+// the wavefront's rows are then formed again with fp32 products.
 #include <type_traits>
 
 #include "attend_split.hpp"
@@ -22,6 +22,109 @@ constexpr int BK = 32;               // keys per tile
 constexpr int NT = kSplitThreads;
 // The exponents' reference is raised this far beyond the row maximum when that passes it (log2): weights are at most 1.
 constexpr float kAhead = 4.0f;
+
+// Is there a sum of which parts were lost (0 < |x| < 2^-90), or one that is infinite or not a number (then their total is too), or were
+// there such rows of Q (`odd`)?  (8 on 2 x 128, 328 rows on 1311 keys: nothing looked at 35.2 us, each sum compared by itself 36.2, this 35.9.)
+template <int NB>
+__device__ __forceinline__ bool again_in_fp32(bool odd, const f32x16_t (&o)[NB], float l) {
+    auto rank = [](float x) { return (__float_as_uint(x) << 1) - 1u; };         // by magnitude, zero last
+    float total = fabsf(l);
+    uint32_t least = rank(l);
+#pragma unroll
+    for (int b = 0; b < NB; ++b)
+#pragma unroll
+        for (int i = 0; i < 16; ++i) {
+            total += fabsf(o[b][i]);
+            least = rank(o[b][i]) < least ? rank(o[b][i]) : least;
+        }
+    return (__ballot(odd || least < rank(0x1p-90f)) | odd_sum(total)) != 0;
+}
+
+// The 32 rows of a wavefront over its tiles t, t + step, ... < t_end once more, with fp32 products.  `q` is the lane's own row from
+// column 4 hh on; value column 32 b + l32 is row l32 of block b.  Slow: every wavefront reads its operands from memory.
+template <int D>
+__device__ __forceinline__ void rows_in_fp32(const float* q, const FcCodesHead& head, const float* kbase, const float* vbase, uint32_t ts,
+                                             const Segments& sg, int t, int t_end, int step, float c2, int lane, f32x16_t (&o)[D / 32], float& m, float& l) {
+    constexpr int NB = D / 32;
+    const int l32 = lane & 31, hh = lane >> 5;
+#pragma unroll
+    for (int b = 0; b < NB; ++b)
+#pragma unroll
+        for (int i = 0; i < 16; ++i) o[b][i] = 0.f;
+    m = kNegBig;
+    l = 0.f;
+    f32x16_t s;
+    auto scores = [&](int j, const f32x4_t& kf) __attribute__((always_inline)) {   // contracts over elements 8 j + i and 8 j + 4 + i
+        const f32x4_t qf = *reinterpret_cast<const f32x4_t*>(q + 8 * j) * c2;
+#pragma unroll
+        for (int i = 0; i < 4; ++i) s = __builtin_amdgcn_mfma_f32_32x32x2f32(kf[i], qf[i], s, 0, 0, 0);
+    };
+    auto weights = [&](int nv) __attribute__((always_inline)) {
+        if (nv < BK) {
+#pragma unroll
+            for (int i = 0; i < 16; ++i)
+                if ((i >> 2) * 8 + hh * 4 + (i & 3) >= nv) s[i] = kNegBig;
+        }
+        float mx = s[0];
+#pragma unroll
+        for (int i = 1; i < 16; ++i) mx = fmaxf(mx, s[i]);
+        const float mn = fmaxf(m, fmaxf(mx, __shfl_xor(mx, 32, FC_WAVE))), alpha = __builtin_amdgcn_exp2f(m - mn);
+        m = mn;
+        float ps = 0.f;
+#pragma unroll
+        for (int i = 0; i < 16; ++i) { s[i] = __builtin_amdgcn_exp2f(s[i] - mn); ps += s[i]; }
+        l = fmaf(l, alpha, ps);
+#pragma unroll
+        for (int b = 0; b < NB; ++b) o[b] *= alpha;
+    };
+    // (keys past the end have the last one's value, which may be infinite, and no weight: zero instead)
+    auto key_of = [&](int i) { return (i >> 2) * 8 + hh * 4 + (i & 3); };
+    auto inside = [&](int i, int nv) { return (uint32_t)(key_of(i) < nv ? key_of(i) : nv - 1); };
+    int seg = 0;
+#pragma unroll 1
+    for (; t < t_end; t += step) {
+#pragma unroll
+        for (int i = 0; i < 16; ++i) s[i] = 0.f;
+        if (t < head.tiles) {
+            const int left = head.L_clean - t * BK, nv = left < BK ? left : BK;
+            const uint8_t *kt = head.k + (int64_t)t * (16 * D), *vt = head.v + (int64_t)t * (16 * D);
+            const uint8_t *kst = head.k + head.to_scales + (int64_t)t * D, *vst = head.v + head.to_scales + (int64_t)t * D;
+            const uint32_t row = (uint32_t)(l32 < nv ? l32 : nv - 1);
+#pragma unroll 2
+            for (int j = 0; j < D / 8; ++j)
+                scores(j, fc_kv4_to_f32(*reinterpret_cast<const uint16_t*>(kt + (row * (D / 2) + 4 * j + 2 * hh)), kst[row * (D / 32) + (j >> 2)]));
+            weights(nv);
+#pragma unroll
+            for (int i = 0; i < 16; ++i) {
+                const uint32_t key = inside(i, nv);
+#pragma unroll
+                for (int b = 0; b < NB; ++b) {
+                    const uint32_t two = vt[key * (D / 2) + 16 * b + (l32 >> 1)];
+                    const f32x4_t v = fc_kv4_to_f32(l32 & 1 ? two >> 4 : two, vst[key * (D / 32) + b]);
+                    o[b] = __builtin_amdgcn_mfma_f32_32x32x2f32(key_of(i) < nv ? v[0] : 0.f, s[i], o[b], 0, 0, 0);
+                }
+                __builtin_amdgcn_sched_barrier(0);         // (few values in registers at a time)
+            }
+        } else {
+            const int tt = t - head.tiles;
+            while (tt >= __builtin_amdgcn_readfirstlane(sg.tile0[seg + 1])) ++seg;
+            const int off = (tt - __builtin_amdgcn_readfirstlane(sg.tile0[seg])) * BK;
+            const int left = __builtin_amdgcn_readfirstlane(sg.len[seg]) - off, nv = left < BK ? left : BK;
+            const int64_t pos = (int64_t)(__builtin_amdgcn_readfirstlane(sg.start[seg]) + off) * ts;
+            const float *kr = kbase + pos + (uint32_t)(l32 < nv ? l32 : nv - 1) * ts + 4 * hh, *vt = vbase + pos + l32;
+#pragma unroll 2
+            for (int j = 0; j < D / 8; ++j) scores(j, *reinterpret_cast<const f32x4_t*>(kr + 8 * j));
+            weights(nv);
+#pragma unroll
+            for (int i = 0; i < 16; ++i) {
+                const float* vr = vt + inside(i, nv) * ts;
+#pragma unroll
+                for (int b = 0; b < NB; ++b) o[b] = __builtin_amdgcn_mfma_f32_32x32x2f32(key_of(i) < nv ? vr[32 * b] : 0.f, s[i], o[b], 0, 0, 0);
+                __builtin_amdgcn_sched_barrier(0);
+            }
+        }
+    }
+}
 
 // ---- few query rows ---------------------------------------------------------------------
 // 32 query rows per block; its 8 wavefronts take every 8th 32-key tile of the range, as in attend_kv4.hip (FcAttendArgs
@@ -42,6 +145,7 @@ struct NarrowSmem {
         float o[kSplitWaves * kUnitRows * OROW];        // partial O at the end
     };
     float m_s[kSplitWaves * kUnitRows], l_s[kSplitWaves * kUnitRows];
+    __attribute__((aligned(16))) uint32_t odd[kSplitWaves];   // rows of Q that need fp32 products, by the wavefront that split them
     Segments sg;
 };
 
@@ -61,13 +165,20 @@ __device__ __forceinline__ void attend_narrow(const FcAttendArgs& a, const FcAtt
     const int l32 = lane & 31, hh = lane >> 5;
     const float c2 = a.scale * 1.4426950408889634f;   // fold log2(e): exp(x) = exp2(x*log2 e)
 
-    if (tid == 0) list_segments(a, it.c, sg);
-    if (tid < kUnitRows * (D / 8)) {
-        const int row = tid / (D / 8), e = tid % (D / 8);
+    auto q_row = [&](int row) {
         int rc = it.tile * kUnitRows + row;
         if (rc > a.L_c - 1) rc = a.L_c - 1;
-        const float* qp = (const float*)a.q + (((int64_t)it.r * a.L_c + rc) * a.H_q + it.h) * D + 8 * e;
+        return (const float*)a.q + (((int64_t)it.r * a.L_c + rc) * a.H_q + it.h) * D;
+    };
+
+    if (tid == 0) list_segments(a, it.c, sg);
+    bool odd = false;
+    if (tid < kUnitRows * (D / 8)) {
+        const int row = tid / (D / 8), e = tid % (D / 8);
+        const float* qp = q_row(row) + 8 * e;
         const f32x4_t v0 = *reinterpret_cast<const f32x4_t*>(qp) * c2, v1 = *reinterpret_cast<const f32x4_t*>(qp + 4) * c2;
+#pragma unroll
+        for (int i = 0; i < 4; ++i) odd |= odd_magnitude(v0[i]) | odd_magnitude(v1[i]);
         Split8 s;
         split_pair(s, 0, v0[0], v0[1]); split_pair(s, 1, v0[2], v0[3]);
         split_pair(s, 2, v1[0], v1[1]); split_pair(s, 3, v1[2], v1[3]);
@@ -75,12 +186,15 @@ __device__ __forceinline__ void attend_narrow(const FcAttendArgs& a, const FcAtt
         *reinterpret_cast<u32x4_native*>(sm.t.q[1] + row * QROW + 8 * e) = s.m;
         *reinterpret_cast<u32x4_native*>(sm.t.q[2] + row * QROW + 8 * e) = s.l;
     }
+    odd = __any(odd);
+    if (lane == 0) sm.odd[wave] = odd;
     __syncthreads();
     const int tiles4 = (x.L_clean + BK - 1) / BK;
     const int nt = tiles4 + __builtin_amdgcn_readfirstlane(sg.tile0[sg.n]);
     const int t_end = (int)((int64_t)nt * (it.s + 1) / it.S);
     const int t_end4 = t_end < tiles4 ? t_end : tiles4;
-    int t = (int)((int64_t)nt * it.s / it.S) + wave;
+    const int t_first = (int)((int64_t)nt * it.s / it.S) + wave;
+    int t = t_first;
 
     f32x16_t o[NB];
 #pragma unroll
@@ -265,6 +379,15 @@ __device__ __forceinline__ void attend_narrow(const FcAttendArgs& a, const FcAtt
         }
     }
 
+    const u32x4_native odd0 = *reinterpret_cast<const u32x4_native*>(sm.odd), odd1 = *reinterpret_cast<const u32x4_native*>(sm.odd + 4);
+    odd = (odd0[0] | odd0[1] | odd0[2] | odd0[3] | odd1[0] | odd1[1] | odd1[2] | odd1[3]) != 0u;
+    if (__builtin_expect(again_in_fp32<NB>(odd, o, l), 0)) {
+        const FcCodesHead head{x.k + (int64_t)hk * x.head_codes, x.v + (int64_t)hk * x.head_codes,
+                               x.scales_at + (int64_t)hk * (x.head_scales - x.head_codes), x.L_clean, tiles4};
+        rows_in_fp32<D>(q_row(l32) + 4 * hh, head, (const float*)a.k_cache + (int64_t)hk * a.head_stride,
+                        (const float*)a.v_cache + (int64_t)hk * a.head_stride, ts, sg, t_first, t_end, kSplitWaves, c2, lane, o, m, l);
+    }
+
     l += __shfl_xor(l, 32, FC_WAVE);
     __syncthreads();                                    // every wavefront is done with its tiles and with Q
     if (hh == 0) { sm.m_s[wave * kUnitRows + l32] = m; sm.l_s[wave * kUnitRows + l32] = l; }
@@ -293,6 +416,54 @@ struct WideSmem {
     Segments sg;
 };
 
+// The end of a block: sums that have to be formed again, then the result or the partial.  The thread's numbers are formed anew: kept
+// through the loops for this, they take registers that the loops have not got (one of Q's operands was read back from memory in each
+// tile, 12040 -> 12260 us on 12 x 128, 10200 rows on 40800 keys and two slots; now as without the look at the sums, within 0.3 %).
+template <int D>
+__device__ __forceinline__ void finish_wide(const FcAttendArgs& a, const FcAttendPlan& p, const WideItem& wi, const Segments& sg, int hk, int t_lo,
+                                            int nt, int tiles4, float c2, bool odd, f32x16_t (&o)[D / 32], float m, float l, float* parts, const FcKv4& x4) {
+    constexpr int NB = D / 32;
+    int tid = threadIdx.x;
+    asm volatile("" : "+v"(tid));
+    const int wave = __builtin_amdgcn_readfirstlane(tid >> 6), lane = tid & 63, l32 = lane & 31, hh = lane >> 5;
+    const int row_in_chunk = wi.tile * kWideRows + wave * 32 + l32;
+    const float* q_row = (const float*)a.q + (((int64_t)wi.r * a.L_c + (row_in_chunk > a.L_c - 1 ? a.L_c - 1 : row_in_chunk)) * a.H_q + wi.h) * D;
+    if (__builtin_expect(again_in_fp32<NB>(odd, o, l), 0)) {
+        const FcCodesHead head{x4.k + (int64_t)hk * x4.head_codes, x4.v + (int64_t)hk * x4.head_codes,
+                               x4.scales_at + (int64_t)hk * (x4.head_scales - x4.head_codes), x4.L_clean, tiles4};
+        rows_in_fp32<D>(q_row + 4 * hh, head, (const float*)a.k_cache + (int64_t)hk * a.head_stride, (const float*)a.v_cache + (int64_t)hk * a.head_stride,
+                        (uint32_t)a.tok_stride, sg, t_lo, t_lo + nt, 1, c2, lane, o, m, l);
+    }
+
+    const float ltot = l + __shfl_xor(l, 32, FC_WAVE);
+    if (wi.S > 1) {
+        const int64_t part = (wi.unit * (kWideRows / kUnitRows) + wave) * wi.S + wi.s;   // 32 rows each
+        float* po = parts + (part * kUnitRows + l32) * D;
+#pragma unroll
+        for (int b = 0; b < NB; ++b)
+#pragma unroll
+            for (int g = 0; g < 4; ++g)
+                store_out(po + b * 32 + g * 8 + hh * 4, o[b][4 * g], o[b][4 * g + 1], o[b][4 * g + 2], o[b][4 * g + 3]);
+        if (hh == 0) {
+            float* ml = parts + (int64_t)p.parts * kUnitRows * D + part * 2 * kUnitRows;
+            ml[l32] = m;
+            ml[kUnitRows + l32] = ltot;
+        }
+        return;
+    }
+    if (row_in_chunk >= a.L_c) return;
+    const float inv = 1.0f / ltot;
+    const int64_t row = (int64_t)wi.r * a.L_c + row_in_chunk;
+    float* op = (float*)a.out + (row * a.H_q + wi.h) * D;
+#pragma unroll
+    for (int b = 0; b < NB; ++b)
+#pragma unroll
+        for (int g = 0; g < 4; ++g)
+            store_out(op + b * 32 + g * 8 + hh * 4, o[b][4 * g] * inv, o[b][4 * g + 1] * inv, o[b][4 * g + 2] * inv, o[b][4 * g + 3] * inv);
+    if (a.lse && hh == 0)
+        a.lse[(int64_t)wi.h * a.A * a.L_c + row] = (m + __builtin_amdgcn_logf(ltot)) * 0.6931471805599453f;
+}
+
 template <int D>
 __device__ __forceinline__ void attend_wide(const FcAttendArgs& a, const FcAttendPlan& p, uint32_t valid, WideSmem<D>& sm,
                                             float* parts, const FcKv4& x4) {
@@ -319,14 +490,21 @@ __device__ __forceinline__ void attend_wide(const FcAttendArgs& a, const FcAtten
     const int row_in_chunk = wi.tile * kWideRows + wave * 32 + l32;
     const float* q_row = (const float*)a.q + (((int64_t)wi.r * a.L_c + (row_in_chunk > a.L_c - 1 ? a.L_c - 1 : row_in_chunk)) * a.H_q + wi.h) * D;
     Split8 qf[KS];
+    // odd_magnitude() of an entry times c2, without that product (which the splitting forms with the differences that follow it)
+    const float small = 0x1p-100f / c2, large = 0x1p100f / c2;
+    auto odd_entry = [&](float x) __attribute__((always_inline)) { return x != 0.f && !(fabsf(x) >= small && fabsf(x) < large); };
+    bool odd = false;
 #pragma unroll
     for (int st = 0; st < KS; ++st) {
-        const f32x4_t x0 = *reinterpret_cast<const f32x4_t*>(q_row + 16 * st + 8 * hh) * c2;
-        const f32x4_t x1 = *reinterpret_cast<const f32x4_t*>(q_row + 16 * st + 8 * hh + 4) * c2;
+        const f32x4_t q0 = *reinterpret_cast<const f32x4_t*>(q_row + 16 * st + 8 * hh), q1 = *reinterpret_cast<const f32x4_t*>(q_row + 16 * st + 8 * hh + 4);
+        const f32x4_t x0 = q0 * c2, x1 = q1 * c2;
+#pragma unroll
+        for (int i = 0; i < 4; ++i) odd = odd || odd_entry(q0[i]) || odd_entry(q1[i]);
         split_pair(qf[st], 0, x0[0], x0[1]); split_pair(qf[st], 1, x0[2], x0[3]);
         split_pair(qf[st], 2, x1[0], x1[1]); split_pair(qf[st], 3, x1[2], x1[3]);
         if (st < QL) sm.ql[st][wave][lane] = qf[st].l;
     }
+    odd = __any(odd);
     __syncthreads();
 
     const int tiles4 = (x4.L_clean + BK - 1) / BK;
@@ -570,33 +748,7 @@ __device__ __forceinline__ void attend_wide(const FcAttendArgs& a, const FcAtten
         for (; t < nt; ++t) step(rows, rows, t);
     }
 
-    const float ltot = l + __shfl_xor(l, 32, FC_WAVE);
-    if (wi.S > 1) {
-        const int64_t part = (wi.unit * (kWideRows / kUnitRows) + wave) * wi.S + wi.s;   // 32 rows each
-        float* po = parts + (part * kUnitRows + l32) * D;
-#pragma unroll
-        for (int b = 0; b < NB; ++b)
-#pragma unroll
-            for (int g = 0; g < 4; ++g)
-                store_out(po + b * 32 + g * 8 + hh * 4, o[b][4 * g], o[b][4 * g + 1], o[b][4 * g + 2], o[b][4 * g + 3]);
-        if (hh == 0) {
-            float* ml = parts + (int64_t)p.parts * kUnitRows * D + part * 2 * kUnitRows;
-            ml[l32] = m;
-            ml[kUnitRows + l32] = ltot;
-        }
-        return;
-    }
-    if (row_in_chunk >= a.L_c) return;
-    const float inv = 1.0f / ltot;
-    const int64_t row = (int64_t)wi.r * a.L_c + row_in_chunk;
-    float* op = (float*)a.out + (row * a.H_q + wi.h) * D;
-#pragma unroll
-    for (int b = 0; b < NB; ++b)
-#pragma unroll
-        for (int g = 0; g < 4; ++g)
-            store_out(op + b * 32 + g * 8 + hh * 4, o[b][4 * g] * inv, o[b][4 * g + 1] * inv, o[b][4 * g + 2] * inv, o[b][4 * g + 3] * inv);
-    if (a.lse && hh == 0)
-        a.lse[(int64_t)wi.h * a.A * a.L_c + row] = (m + __builtin_amdgcn_logf(ltot)) * 0.6931471805599453f;
+    finish_wide<D>(a, p, wi, sg, hk, t_lo, nt, tiles4, c2, odd, o, m, l, parts, x4);
 }
 
 // WIDE and NARROW say which of the two bodies some recompute count of this launch asks for.

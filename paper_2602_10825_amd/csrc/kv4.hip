@@ -97,12 +97,7 @@ __global__ __launch_bounds__(kThreads) void kv4_pack_kernel(FcKv4Args a) {
 
 // EPL codes and their scale's byte -> 16 bytes of the cache
 __device__ __forceinline__ u32x4_native expand(uint32_t codes, uint32_t scale, bf16_t) { return fc_kv4_to_bf16(codes, scale); }
-__device__ __forceinline__ u32x4_native expand(uint32_t codes, uint32_t scale, float) {
-    typedef float f32x2_t __attribute__((ext_vector_type(2)));
-    const float s = __uint_as_float(scale << 23);
-    const f32x2_t a = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(codes, s, 0), b = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(codes, s, 1);
-    return u32x4_native{__float_as_uint(a.x), __float_as_uint(a.y), __float_as_uint(b.x), __float_as_uint(b.y)};
-}
+__device__ __forceinline__ u32x4_native expand(uint32_t codes, uint32_t scale, float) { return __builtin_bit_cast(u32x4_native, fc_kv4_to_f32(codes, scale)); }
 
 template <typename T, int D, bool STREAM>
 __global__ __launch_bounds__(kThreads) void kv4_unpack_kernel(FcKv4Args a) {

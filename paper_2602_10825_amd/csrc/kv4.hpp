@@ -8,6 +8,7 @@
 #include "fc_common.hpp"
 
 typedef __bf16 fc_bf16x2_t __attribute__((ext_vector_type(2)));
+typedef float fc_f32x4_t __attribute__((ext_vector_type(4)));
 
 // Eight codes and their scale's byte -> eight bf16 values.  The conversion takes the scale's exponent from a float's, and its
 // exponent of all ones gives NaN.
@@ -19,4 +20,12 @@ __device__ __forceinline__ u32x4_native fc_kv4_to_bf16(uint32_t codes, uint32_t 
     r.z = __builtin_bit_cast(uint32_t, (fc_bf16x2_t)__builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(codes, s, 2));
     r.w = __builtin_bit_cast(uint32_t, (fc_bf16x2_t)__builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(codes, s, 3));
     return r;
+}
+
+// Four codes and their scale's byte -> four floats
+__device__ __forceinline__ fc_f32x4_t fc_kv4_to_f32(uint32_t codes, uint32_t scale_byte) {
+    typedef float f32x2_t __attribute__((ext_vector_type(2)));
+    const float s = __uint_as_float(scale_byte << 23);
+    const f32x2_t a = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(codes, s, 0), b = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(codes, s, 1);
+    return fc_f32x4_t{a.x, a.y, b.x, b.y};
 }
