@@ -686,19 +686,11 @@ __global__ __launch_bounds__(NT) void attend_kv4_kernel(FcAttendArgs a, FcAttend
         attend_narrow4<D>(a, p, valid, *reinterpret_cast<Narrow4Smem<D>*>(raw), parts, x);
 }
 
-// The plan's costs, from times of both bodies with forced numbers of ranges.  A 32-key tile costs a 32-row block two thirds of
-// what it costs with a bf16 cache, so that body is taken more often: 24 x 64, 278 rows on 20000 keys narrow 69 / wide 90 us;
-// 12 x 128, 600 rows on 20000 102 / 105, 256 rows on 49201 124 / 92, 12 x 64, 2 x 174 rows on 18406 55 / 50.
-FcAttendPlan plan_kv4(const FcAttendArgs& a, int L_clean, bool may_split) {
-    return fc_attend_plan(a.A, a.L_c, L_clean, a.H_q, may_split, a.d == 128 ? FcAttendCosts{1.6, 5.0, 5.0, 14.0, 0.0, 0.155, 16, false}
-                                                                            : FcAttendCosts{1.15, 5.0, 5.0, 8.0, 0.0, 0.105, 16, false});
-}
-
 template <int D>
 int launch_kv4(FcAttendArgs a, const FcKv4& x, hipStream_t s) {
     a.L_clean = 0;                    // the slots alone
-    FcAttendPlan p = plan_kv4(a, x.L_clean, true);
-    if (!fc_room_for_partials(a.ws, a.ws_bytes, p.parts, D)) p = plan_kv4(a, x.L_clean, false);
+    FcAttendPlan p = fc_attend_plan_kv4(a.A, a.L_c, x.L_clean, a.H_q, D, true);
+    if (!fc_room_for_partials(a.ws, a.ws_bytes, p.parts, D)) p = fc_attend_plan_kv4(a.A, a.L_c, x.L_clean, a.H_q, D, false);
     bool wide = false, narrow = false;
     for (int R = 0; R < a.A; ++R) (p.narrow[R] ? narrow : wide) = true;
     if (!narrow)

@@ -765,19 +765,11 @@ __global__ __launch_bounds__(NT) void attend_kv4_f32_kernel(FcAttendArgs a, FcAt
         attend_narrow<D>(a, p, valid, *reinterpret_cast<NarrowSmem<D>*>(raw), parts, x);
 }
 
-// The plan's costs, those of a tile of codes and of a slot's in the proportion of the newest chunk's keys.
-FcAttendPlan plan_of(const FcAttendArgs& a, int L_clean, bool may_split) {
-    const double slots = (double)a.A * a.L_c, f = L_clean / (L_clean + slots);
-    auto mix = [&](double of_codes, double of_rows) { return f * of_codes + (1.0 - f) * of_rows; };
-    return fc_attend_plan(a.A, a.L_c, L_clean, a.H_q, may_split, a.d == 128 ? FcAttendCosts{mix(4.7, 9.0), 8.0, 5.0, 16.0, 0.5, mix(0.32, 0.65), 10, true}
-                                                                            : FcAttendCosts{mix(3.2, 5.2), 6.0, 5.0, 8.0, 0.5, mix(0.20, 0.40), 14, true});
-}
-
 template <int D>
 int launch(FcAttendArgs a, const FcKv4& x, hipStream_t s) {
     a.L_clean = 0;                    // the slots alone
-    FcAttendPlan p = plan_of(a, x.L_clean, true);
-    if (!fc_room_for_partials(a.ws, a.ws_bytes, p.parts, D)) p = plan_of(a, x.L_clean, false);
+    FcAttendPlan p = fc_attend_plan_kv4_f32(a.A, a.L_c, x.L_clean, a.H_q, D, true);
+    if (!fc_room_for_partials(a.ws, a.ws_bytes, p.parts, D)) p = fc_attend_plan_kv4_f32(a.A, a.L_c, x.L_clean, a.H_q, D, false);
     bool wide = false, narrow = false;
     for (int R = 0; R < a.A; ++R) (p.narrow[R] ? narrow : wide) = true;
     if (!narrow)

@@ -135,6 +135,21 @@ inline FcAttendPlan fc_attend_plan_f32(int A, int L_c, int L_clean, int H_q, boo
                                                                     : FcAttendCosts{4.5, 6.0, 5.0, 8.0, 0.5, 0.42, 8, true});
 }
 
+// A clean region in 4 bits, bf16: a 32-key tile costs a 32-row block two thirds of what it costs with a bf16 cache, so that body is taken
+// more often.  24 x 64, 278 rows on 20000 keys narrow 69 / wide 90; 12 x 128, 600 rows on 20000 102 / 105, 256 rows on 49201 124 / 92,
+// 12 x 64, 2 x 174 rows on 18406 55 / 50 (times of the fit, before the merge went from 6.4 to 4.0 us).
+inline FcAttendPlan fc_attend_plan_kv4(int A, int L_c, int L_clean, int H_q, int d, bool may_split) {
+    return fc_attend_plan(A, L_c, L_clean, H_q, may_split, d == 128 ? FcAttendCosts{1.6, 5.0, 5.0, 14.0, 0.0, 0.155, 16, false}
+                                                                    : FcAttendCosts{1.15, 5.0, 5.0, 8.0, 0.0, 0.105, 16, false});
+}
+// ... and fp32: the costs of a tile of codes and of a slot's in the proportion of the newest chunk's keys.
+inline FcAttendPlan fc_attend_plan_kv4_f32(int A, int L_c, int L_clean, int H_q, int d, bool may_split) {
+    const double slots = (double)A * L_c, f = L_clean / (L_clean + slots);
+    auto mix = [&](double of_codes, double of_rows) { return f * of_codes + (1.0 - f) * of_rows; };
+    return fc_attend_plan(A, L_c, L_clean, H_q, may_split, d == 128 ? FcAttendCosts{mix(4.7, 9.0), 8.0, 5.0, 16.0, 0.5, mix(0.32, 0.65), 10, true}
+                                                                    : FcAttendCosts{mix(3.2, 5.2), 6.0, 5.0, 8.0, 0.5, mix(0.20, 0.40), 14, true});
+}
+
 // Most 32-row partials a launch with these shapes can need, whatever the number of keys.  The wide
 // plan takes S only where the last round costs less than with every smaller S'.  Both costs are a + b T
 // in the number of tiles T and a never falls with S (more rounds of blocks, a merge), so b, the rounds of
