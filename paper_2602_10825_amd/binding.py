@@ -462,17 +462,21 @@ def _same_device(call: str, stream, *tensors: Optional[torch.Tensor]) -> None:
             raise ValueError(f"{call}: a tensor on {t.device}, the stream on cuda:{on}")
 
 
-def _check_ints(call: str, *xs: int) -> None:
-    """The library takes them as int: what lies beyond would be cut to 32 bits."""
-    if max(xs) > 0x7fffffff or min(xs) < -0x80000000:
-        raise ValueError(f"{call}: a number beyond 32 bits among {xs}")
+_I32 = torch.int32
+
+
+def _check_ints(call: str, bits: int) -> None:
+    """The library takes numbers as int: what lies beyond would be cut to 32 bits.  ``bits`` is all of a call's numbers, or-ed (a negative
+    one hides the others, and the library refuses it)."""
+    if bits >> 31 not in (0, -1):
+        raise ValueError(f"{call}: a number beyond 32 bits")
 
 
 def _check_lists(call: str, recompute_idx: torch.Tensor, n_recompute: torch.Tensor) -> None:
     """The kernels read the recompute list by address: entries of another type would be other chunks."""
-    for x in (recompute_idx, n_recompute):
-        if x.dtype != torch.int32 or not x.is_contiguous():
-            raise ValueError(f"{call}: recompute_idx and n_recompute are contiguous int32, got strides {x.stride()} of {x.dtype}")
+    if recompute_idx.dtype is not _I32 or n_recompute.dtype is not _I32 or not (recompute_idx.is_contiguous() and n_recompute.is_contiguous()):
+        raise ValueError(f"{call}: recompute_idx and n_recompute are contiguous int32, got {recompute_idx.dtype} with strides "
+                         f"{recompute_idx.stride()} and {n_recompute.dtype} with strides {n_recompute.stride()}")
 
 
 _PAIRINGS = {"interleaved": 0, "halves": 1}
@@ -516,7 +520,8 @@ def flowcache_qk_norm_rope(q: torch.Tensor, k: torch.Tensor, v: Optional[torch.T
         raise ValueError(f"{call}: pairing is one of {sorted(_PAIRINGS)}, got {pairing!r}")
     _same_device(call, stream, q, k, v, k_cache, v_cache, recompute_idx, n_recompute, q_weight, k_weight, q_out)
     _check_lists(call, recompute_idx, n_recompute)
-    _check_ints(call, L_clean, *grid)
+    L_clean, grid_h, grid_w = int(L_clean), int(grid[0]), int(grid[1])
+    _check_ints(call, L_clean | grid_h | grid_w)
     qs = _heads_of_rows(call, "q", q, rows, H_q, d, dtype)
     ks = _heads_of_rows(call, "k", k, rows, H_k, d, dtype)
     strides = k_cache.stride()
@@ -535,8 +540,8 @@ def flowcache_qk_norm_rope(q: torch.Tensor, k: torch.Tensor, v: Optional[torch.T
     st = (_lib or lib()).flowcache_qk_norm_rope(
         q.data_ptr(), qs, k.data_ptr(), _ptr(v), ks, _dtype_code(k_cache), H_q, H_k, d, int(norm_eps is not None),
         0.0 if norm_eps is None else float(norm_eps), _ptr(q_weight), _ptr(k_weight), _ints(dims),
-        _PAIRINGS[pairing], float(theta), int(grid[0]), int(grid[1]), _ints(frame0), int(L_c),
-        int(L_clean), A, _ints(active_off), recompute_idx.data_ptr(), n_recompute.data_ptr(),
+        _PAIRINGS[pairing], float(theta), grid_h, grid_w, _ints(frame0), int(L_c),
+        L_clean, A, _ints(active_off), recompute_idx.data_ptr(), n_recompute.data_ptr(),
         q_out.data_ptr(), k_cache.data_ptr(), _ptr(v_cache), strides[0], strides[1], capacity, _stream(stream))
     _check(call, st)
     return q_out
@@ -544,8 +549,9 @@ def flowcache_qk_norm_rope(q: torch.Tensor, k: torch.Tensor, v: Optional[torch.T
 
 def kv4_buffer(H_k: int, capacity4: int, d: int, device="cuda") -> torch.Tensor:
     """A buffer for ``capacity4`` rows per head of K or V in 4 bits."""
-    _check_ints("flowcache_kv4_bytes", H_k, capacity4, d)
-    nbytes = (_lib or lib()).flowcache_kv4_bytes(int(H_k), int(capacity4), int(d))
+    H_k, capacity4, d = int(H_k), int(capacity4), int(d)
+    _check_ints("flowcache_kv4_bytes", H_k | capacity4 | d)
+    nbytes = (_lib or lib()).flowcache_kv4_bytes(H_k, capacity4, d)
     if nbytes == 0:
         raise FlowCacheError("flowcache_kv4_bytes", FC_INVALID_ARGUMENT)
     return torch.empty(nbytes, dtype=torch.uint8, device=device)
@@ -555,7 +561,7 @@ def _kv4_shapes(call: str, k4, v4, capacity4: int, k_cache, v_cache) -> tuple:
     shape, strides = k_cache.shape, k_cache.stride()
     assert strides[2] == 1 and (v4 is None) == (v_cache is None)
     assert v_cache is None or (v_cache.stride() == strides and v_cache.shape == shape and v_cache.dtype == k_cache.dtype)
-    need = shape[0] * int(capacity4) * (shape[2] // 2 + shape[2] // 32)
+    need = shape[0] * capacity4 * (shape[2] // 2 + shape[2] // 32)
     for x in (k4, v4):
         if x is not None and (x.dtype != torch.uint8 or not x.is_contiguous() or x.numel() < need):
             raise ValueError(f"{call}: a 4-bit buffer of {capacity4} rows per head is {need} contiguous bytes of uint8")
@@ -570,12 +576,13 @@ def flowcache_kv4_pack(k_cache: torch.Tensor, v_cache: Optional[torch.Tensor], k
     call = "flowcache_kv4_pack"
     H_k, capacity, d = k_cache.shape
     _same_device(call, stream, k_cache, v_cache, k4, v4, kept_idx)
-    _check_ints(call, capacity4, count, cache_pos, pos4)
+    capacity4, count, cache_pos, pos4 = int(capacity4), int(count), int(cache_pos), int(pos4)
+    _check_ints(call, capacity4 | count | cache_pos | pos4)
     strides = _kv4_shapes(call, k4, v4, capacity4, k_cache, v_cache)
     assert kept_idx is None or (kept_idx.dtype == torch.int32 and kept_idx.is_contiguous() and kept_idx.shape == (H_k, count))
     st = (_lib or lib()).flowcache_kv4_pack(_ptr(k_cache), _ptr(v_cache), strides[0], strides[1], capacity,
-                                            _dtype_code(k_cache), H_k, d, int(cache_pos), _ptr(kept_idx), int(count),
-                                            _ptr(k4), _ptr(v4), int(capacity4), int(pos4), _stream(stream))
+                                            _dtype_code(k_cache), H_k, d, cache_pos, _ptr(kept_idx), count,
+                                            _ptr(k4), _ptr(v4), capacity4, pos4, _stream(stream))
     _check(call, st)
 
 
@@ -586,11 +593,12 @@ def flowcache_kv4_unpack(k4: torch.Tensor, v4: Optional[torch.Tensor], capacity4
     call = "flowcache_kv4_unpack"
     H_k, capacity, d = k_cache.shape
     _same_device(call, stream, k_cache, v_cache, k4, v4)
-    _check_ints(call, capacity4, count, cache_pos, pos4)
+    capacity4, count, cache_pos, pos4 = int(capacity4), int(count), int(cache_pos), int(pos4)
+    _check_ints(call, capacity4 | count | cache_pos | pos4)
     strides = _kv4_shapes(call, k4, v4, capacity4, k_cache, v_cache)
-    st = (_lib or lib()).flowcache_kv4_unpack(_ptr(k4), _ptr(v4), int(capacity4), int(pos4), int(count), _ptr(k_cache),
+    st = (_lib or lib()).flowcache_kv4_unpack(_ptr(k4), _ptr(v4), capacity4, pos4, count, _ptr(k_cache),
                                               _ptr(v_cache), strides[0], strides[1], capacity, _dtype_code(k_cache),
-                                              H_k, d, int(cache_pos), _stream(stream))
+                                              H_k, d, cache_pos, _stream(stream))
     _check(call, st)
 
 
@@ -608,7 +616,8 @@ def flowcache_attend_kv4(q: torch.Tensor, k_new: Optional[torch.Tensor], v_new: 
     A = len(active_off)
     _same_device(call, stream, q, k_cache, v_cache, k_new, v_new, k4, v4, recompute_idx, n_recompute, out, workspace)
     _check_lists(call, recompute_idx, n_recompute)
-    _check_ints(call, L_clean, capacity4)
+    L_clean, capacity4 = int(L_clean), int(capacity4)
+    _check_ints(call, L_clean | capacity4)
     assert q.is_contiguous() and rows == A * L_c and k_cache.shape[2] == d and (k4 is None) == (v4 is None)
     assert q.dtype == k_cache.dtype and v_cache is not None
     for x in (k_new, v_new):
@@ -626,9 +635,9 @@ def flowcache_attend_kv4(q: torch.Tensor, k_new: Optional[torch.Tensor], v_new: 
     L = _lib or lib()
     if workspace is None:
         workspace = _workspace(L.flowcache_attend_kv4_workspace(A, L_c, H_q, d), q.device, stream)
-    st = L.flowcache_attend_kv4(_ptr(q), _ptr(k_new), _ptr(v_new), _ptr(k4), _ptr(v4), int(capacity4), _ptr(k_cache),
+    st = L.flowcache_attend_kv4(_ptr(q), _ptr(k_new), _ptr(v_new), _ptr(k4), _ptr(v4), capacity4, _ptr(k_cache),
                                 _ptr(v_cache), strides[0], strides[1], capacity, _dtype_code(q), H_q, H_k, d, int(L_c),
-                                int(L_clean), A, _ints(active_off), _ptr(recompute_idx),
+                                L_clean, A, _ints(active_off), _ptr(recompute_idx),
                                 _ptr(n_recompute), float(softmax_scale), _ptr(out), _ptr(lse), _ptr(workspace),
                                 workspace.numel(), _stream(stream))
     _check(call, st)
