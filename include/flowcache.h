@@ -370,7 +370,9 @@ size_t flowcache_kv_compress_status_offset(int H_k, int L_k, int d, int budget, 
  * may end inside a frame.  The head's d / 2 pairs are dealt to the axes in that order: the first
  * dims[0] / 2 turn with time, the next dims[1] / 2 with height, the next dims[2] / 2 with width, and
  * what is left does not turn.  Pair i of an axis turns by  position * theta^(-2 i / dims[axis]).
- * Elements are widened to float32, worked on in float32 (angles in float64) and rounded once.
+ * Elements are widened to float32, worked on in float32 (angles beyond float64) and rounded once; heads of
+ * any magnitude are normalised.  The norm is each head's own: one over all heads of a token is another
+ * (norm = 0 here).
  *
  *   q        [dev] rows of H_q heads of d elements (a head's elements and a row's heads follow each
  *                  other); row block r (L_c rows) <-> chunk recompute_idx[r]; row to row q_tok_stride
@@ -411,7 +413,8 @@ int flowcache_qk_norm_rope(const void* q, int64_t q_tok_stride, const void* k, c
  *     codes   [H_k, capacity4, d / 2]   two a byte, the even element in the low half; bit 3 the sign, bits
  *                                       0-2 the index into the eight magnitudes
  *     scales  [H_k, capacity4, d / 32]  the bytes b (255: the 32 elements are not numbers)
- * Every value is exact in float32, and in bfloat16.
+ * Every value is exact in float32, and in bfloat16 (of bytes 253 and 254, which packing does not write, the
+ * largest are infinities there).
  *
  * flowcache_kv4_pack turns `count` rows of every head into 4 bits, at positions pos4 .. of the buffers:
  * those at cache_pos .., or, with kept_idx, rows kept_idx[h][0 .. count) of head h (as written by

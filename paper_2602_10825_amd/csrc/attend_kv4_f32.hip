@@ -2,11 +2,11 @@
 // the bf16 matrix cores, floats in three bf16 parts (f32_split.hpp).  A value of the 4-bit rows has two significant
 // bits and is its own first part, so a product with it takes three of the six: a clean key costs half of
 // what it costs attend_f32.hip, which also reads 16 times its bytes.  Bodies, plan and divisions of the keys as there.
-// us, attend_f32.hip on the unpacked rows / here: 12 x 128, one row on 61201 keys 200 / 47, 256 rows on 49201 372 / 211, 600 on 5200
-// 134 / 78, 10200 on 40800 keys and two slots 16600 / 11830; 24 x 128, 2 chunks of 4000 rows on 20000 keys 10870 / 7440, 4 of 2340 on
-// their slots alone 3360 / 3240; 24 x 64, 2 of 2040 rows on 18360 keys and 5 slots 3040 / 2440.
-// The large ones run at 325 .. 380 TFLOP/s counted as fp32, where a third (codes) and a sixth (slots) of a large bf16 product's rate are
-// 394 and 197: matrix cores.
+// us, attend_f32.hip on the unpacked rows / here, three sets of inputs in turn (no cache is found in the Infinity Cache): 12 x 128, one
+// row on 61201 keys 193 / 45, 256 rows on 49201 388 / 227, 600 on 5200 140 / 78, 10200 on 40800 keys and two slots 16630 / 12390; 24 x 128,
+// 2 chunks of 4000 rows on 20000 keys 11020 / 7750, 4 of 2340 on their slots alone 3520 / 3450; 24 x 64, 2 of 2040 rows on 18360 keys and
+// 5 slots 3180 / 2560.  The large ones run at 309 and 330 TFLOP/s counted as fp32; a third (codes) and a sixth (slots) of a large bf16
+// product's rate on that card, mixed as their keys are, 340 and 366: matrix cores.
 //
 // What has no parts or loses them (infinities, entries near the largest float, very small ones) is looked for in Q and in the sums, and
 // the wavefront's rows are then formed again with fp32 products.
