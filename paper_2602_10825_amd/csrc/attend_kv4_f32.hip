@@ -23,13 +23,17 @@ constexpr int NT = kSplitThreads;
 // The exponents' reference is raised this far beyond the row maximum when that passes it (log2): weights are at most 1.
 constexpr float kAhead = 4.0f;
 
-// Is there a sum of which parts were lost (0 < |x| < 2^-90), or one that is infinite or not a number (then their total is too), or were
-// there such rows of Q (`odd`)?  (8 on 2 x 128, 328 rows on 1311 keys: nothing looked at 35.2 us, each sum compared by itself 36.2, this 35.9.)
+// Is there a sum of products of which parts were lost, or one that is infinite or not a number (then their total is too), or were there
+// such rows of Q (`odd`)?  What a value or a weight loses is at most 2^-134 (half of bf16's least step), so a sum over all keys loses at
+// most 2^-134 times the sum of weights: less than 2^-24 of it from 2^-110 times that sum on.  Zeros lost nothing.  (A key that
+// outweighs all others by 76 in natural units and has zeros among its codes leaves such sums too; with a border of 2^-90 and the
+// sums of weights looked at as well it was 62: 256 rows on 8000 keys, 16 of them 70 above the others, 63 us, and 160 then.
+// 8 on 2 x 128, 328 rows on 1311 keys: nothing looked at 35.2 us, each sum compared by itself 36.2, this 35.9.)
 template <int NB>
 __device__ __forceinline__ bool again_in_fp32(bool odd, const f32x16_t (&o)[NB], float l) {
     auto rank = [](float x) { return (__float_as_uint(x) << 1) - 1u; };         // by magnitude, zero last
     float total = fabsf(l);
-    uint32_t least = rank(l);
+    uint32_t least = ~0u;
 #pragma unroll
     for (int b = 0; b < NB; ++b)
 #pragma unroll
@@ -37,7 +41,8 @@ __device__ __forceinline__ bool again_in_fp32(bool odd, const f32x16_t (&o)[NB],
             total += fabsf(o[b][i]);
             least = rank(o[b][i]) < least ? rank(o[b][i]) : least;
         }
-    return (__ballot(odd || least < rank(0x1p-90f)) | odd_sum(total)) != 0;
+    const float weights = l + __shfl_xor(l, 32, FC_WAVE);
+    return (__ballot(odd || least < rank(weights * 0x1p-110f)) | odd_sum(total)) != 0;
 }
 
 // The 32 rows of a wavefront over its tiles t, t + step, ... < t_end once more, with fp32 products.  `q` is the lane's own row from

@@ -52,7 +52,7 @@ class Case:
         self.k, self.v = (normal(rng, self.H_k, rows, self.d) for _ in range(2))
         self.scale = 0.25 * self.d ** -0.5                    # (a code's root mean square is about 3)
 
-    def check(self, k_ref=None, room=True):
+    def check(self, k_ref=None, room=True, bar=1e-5, least_weight=0.0):
         dtype, A, L_c, L, d = self.dtype, self.A, self.L_c, self.L, self.d
         q, k, v = (torch.from_numpy(x.astype(np.float32)).to(DEV).to(dtype) for x in (self.q, self.k, self.v))
         idx, n, off = torch.arange(A, dtype=torch.int32, device=DEV), torch.tensor([A], dtype=torch.int32, device=DEV), [i * L_c for i in range(A)]
@@ -75,8 +75,8 @@ class Case:
                 lse_tol = torch.full_like(want_lse, 2.0 ** -8 + 1e-5)
             else:
                 row = (qq.abs() @ kk.abs().transpose(1, 2).contiguous()).amax(-1) * scale
-                u = (2.0 ** -24 * (2 * 132 * row + 60 + 2 * s.shape[-1])).clamp(max=1e-5)
-                tol, lse_tol = 2.0 ** -24 * want.abs() + u[..., None] * size + 2.0 ** -149 * s.shape[-1], u + 2.0 ** -23 * want_lse.abs()
+                u = (2.0 ** -24 * (2 * 132 * row + 60 + 2 * s.shape[-1])).clamp(max=bar)
+                tol, lse_tol = 2.0 ** -24 * want.abs() + u[..., None] * size + 2.0 ** -149 * s.shape[-1] + least_weight * vv.abs().sum(1, keepdim=True), u + 2.0 ** -23 * want_lse.abs()
             inf = want.to(F32 if dtype == F32 else BF).isinf()
             have = self.out[blk].transpose(0, 1)
             assert torch.equal(have[inf], want[inf].to(have.dtype).sign() * float("inf"))
@@ -167,7 +167,7 @@ def test_channels_of_opposite_magnitude(shape):
 
 
 @pytest.mark.parametrize("shape", SHAPES)
-@pytest.mark.parametrize("power", [24, 60, 100, -100, -118, -140])
+@pytest.mark.parametrize("power", [24, 60, 100, -100, -106, -110, -112, -115, -118, -130, -140])
 def test_a_value_column_of_another_magnitude(shape, power):
     """In the slots alone, and with the clean rows' values so small that only the column's own size counts."""
     case = Case(shape, F32, 9)
